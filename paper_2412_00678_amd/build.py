@@ -22,7 +22,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall", "-Wno-unused-value",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # scan2d_api.hip is compiled last: it includes the register table generated from the remarks of the forward units
-UNITS = ["scan2d_elementwise.hip", "scan2d_block.hip", "scan2d_xproj.hip", "scan2d_pool.hip", "scan2d_linear.hip", "scan2d_norm.hip", "scan2d_fwd_f32.hip", "scan2d_fwd_bf16.hip", "scan2d_fwd_f32_sp.hip", "scan2d_fwd_bf16_sp.hip", "scan2d_fwd_f32_um.hip", "scan2d_fwd_bf16_um.hip", "scan2d_fwd_bf16_ua.hip", "scan2d_fwd_f32_sp_um.hip", "scan2d_fwd_bf16_sp_um.hip", "scan2d_fwd_bf16_sp_ua.hip",
+UNITS = ["scan2d_elementwise.hip", "scan2d_block.hip", "scan2d_xproj.hip", "scan2d_pool.hip", "scan2d_linear.hip", "scan2d_norm.hip", "scan2d_recur.hip", "scan2d_group_norm.hip", "scan2d_seq_api.hip", "scan2d_fwd_f32.hip", "scan2d_fwd_bf16.hip", "scan2d_fwd_f32_sp.hip", "scan2d_fwd_bf16_sp.hip", "scan2d_fwd_f32_um.hip", "scan2d_fwd_bf16_um.hip", "scan2d_fwd_bf16_ua.hip", "scan2d_fwd_f32_sp_um.hip", "scan2d_fwd_bf16_sp_um.hip", "scan2d_fwd_bf16_sp_ua.hip",
          "scan2d_fwd_shared_f32.hip", "scan2d_fwd_shared_bf16.hip", "scan2d_fwd_shared_gate.hip", "scan2d_fwd_skew.hip", "scan2d_fwd_shared_f32_cf.hip", "scan2d_fwd_shared_bf16_cf.hip", "scan2d_fwd_av.hip", "scan2d_fwd_tile16.hip", "scan2d_fwd_quads_f32.hip", "scan2d_fwd_quads_bf16.hip",
          "scan2d_bwd.hip", "scan2d_bwd_f32.hip", "scan2d_bwd_bf16.hip", "scan2d_bwd_f32_sp.hip", "scan2d_bwd_bf16_sp.hip",
          "scan2d_bwd_shared_f32.hip", "scan2d_bwd_shared_bf16.hip", "scan2d_bwd_shared_f32_cf.hip", "scan2d_bwd_shared_bf16_cf.hip", "scan2d_bwd_av.hip"]
@@ -168,7 +168,7 @@ def build(force: bool = True, jobs: int = 6, verbose: bool = True) -> str:
     objs = [os.path.join(OBJ, u.replace(".hip", ".o")) for u in UNITS + [API_UNIT]]
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
     src = os.path.join(CSRC, PY_UNIT)
-    if force or not os.path.exists(PY_LIB) or os.path.getmtime(PY_LIB) < max(os.path.getmtime(src), os.path.getmtime(os.path.join(HERE, "..", "include", "scan2d.h"))):
+    if force or not os.path.exists(PY_LIB) or os.path.getmtime(PY_LIB) < max(os.path.getmtime(src), *(os.path.getmtime(os.path.join(HERE, "..", "include", h)) for h in ("scan2d.h", "scan2d_seq.h"))):
         out = _run(_py_extension_cmd())
         if verbose and out.strip():
             print(out)

@@ -19,6 +19,7 @@
 #include "scan2d_block.hpp"
 #include "scan2d_memo.hpp"
 #include "scan2d_tuning.hpp"
+#include "scan2d_seq.hpp"
 
 namespace scan2d {
 
@@ -72,6 +73,7 @@ namespace {
 
 constexpr int kMaxDevices = 64;
 std::atomic<int> g_device_ok[kMaxDevices];   // 0 = unknown, 1 = gfx950, -1 = something else
+}  // namespace
 
 int check_device() {
     int dev = 0;
@@ -86,6 +88,8 @@ int check_device() {
     }
     return st == 1 ? SCAN2D_OK : SCAN2D_ERR_UNSUPPORTED_DEVICE;
 }
+
+namespace {
 
 int check_desc(const scan2d_desc* d) {
     if (d == nullptr) return SCAN2D_ERR_NULL_POINTER;

@@ -8,14 +8,17 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
 #include <utility>
+#include <vector>
 
 #include "../../include/scan2d.h"
+#include "../../include/scan2d_seq.h"
 
 namespace {
 
@@ -375,6 +378,269 @@ PyObject* block_attn_pool(Args a) {       // h, V, w, mask, out
     return tuple(z, attn);
 }
 
+// ---- the sequence layers: channels-last rows
+// A tensor [..., C] whose channels are neighbours and whose rows lie at one stride (the halves of a projection do).
+struct Rows {
+    void* p = nullptr;
+    int64_t stride = 0, rows = 1, C = 0;
+    Rows() = default;
+    explicit Rows(const at::Tensor& v, const char* name) {
+        const int64_t n = v.dim();
+        C = v.size(n - 1);
+        for (int64_t k = 0; k + 1 < n; ++k) rows *= v.size(k);
+        p = v.data_ptr();
+        if (v.numel() == 0) return;
+        bool fits = C == 1 || v.stride(n - 1) == 1;
+        int64_t span = 0;                          // stride of the whole of the dimensions seen so far
+        for (int64_t k = n - 2; k >= 0; --k) {
+            if (v.size(k) == 1) continue;
+            if (stride == 0) stride = span = v.stride(k);
+            else if (v.stride(k) != span) fits = false;
+            span *= v.size(k);
+        }
+        if (stride != 0 && stride < C) fits = false;
+        if (rows > 1 && stride == 0) fits = false;              // one row read for all
+        if (!fits) raise(PyExc_ValueError, std::string(name) + " must have its channels next to each other and its rows at one stride");
+    }
+};
+
+// The row tensor a call is described by, and what all other tensors are checked against.
+struct Seq {
+    at::Tensor x;
+    at::ScalarType t;
+    at::Device dev;
+    std::vector<int64_t> shape;
+    int64_t C, rows;
+    c10::DeviceGuard guard;
+    static const at::Tensor& main(PyObject* o, const char* name, int least) {
+        const at::Tensor& v = tensor(o, name);
+        if (v.dim() < least) raise(PyExc_ValueError, std::string(name) + ": expected at least " + std::to_string(least) + " dimensions, got " + std::to_string(v.dim()));
+        if (!v.is_cuda()) raise(PyExc_ValueError, std::string(name) + " must be a device tensor");
+        if (v.scalar_type() != at::kFloat && v.scalar_type() != at::kBFloat16)
+            raise(PyExc_TypeError, std::string(name) + " must be float32 or bfloat16, got " + describe(v.scalar_type(), {}).substr(0, describe(v.scalar_type(), {}).size() - 3));
+        if (v.size(v.dim() - 1) < 1 || v.size(v.dim() - 1) > 0x7fffffff) raise(PyExc_ValueError, std::string(name) + ": channels out of range");
+        return v;
+    }
+    Seq(PyObject* o, const char* name, int least)
+        : x(main(o, name, least)), t(x.scalar_type()), dev(x.device()), shape(x.sizes().vec()), C(shape.back()), rows(1), guard(dev) {
+        for (size_t k = 0; k + 1 < shape.size(); ++k) rows *= shape[k];
+    }
+    const at::Tensor& here(PyObject* o, const char* name) const {
+        if (o == Py_None) raise(PyExc_ValueError, std::string(name) + " is required");
+        const at::Tensor& v = tensor(o, name);
+        if (!v.is_cuda() || v.device() != dev) raise(PyExc_ValueError, std::string(name) + " must be on the device of the rows");
+        return v;
+    }
+    Rows like(PyObject* o, const char* name) const {          // the shape and type of the main tensor
+        const at::Tensor& v = here(o, name);
+        if (v.scalar_type() != t || v.sizes() != at::IntArrayRef(shape))
+            raise(PyExc_ValueError, std::string(name) + ": expected " + describe(t, shape) + ", got " + describe(v.scalar_type(), v.sizes()));
+        return Rows(v, name);
+    }
+    void* dense(PyObject* o, const char* name, at::ScalarType type, at::IntArrayRef sizes) const {
+        here(o, name);
+        return need(o, name, type, sizes);
+    }
+    void* dense_or_null(PyObject* o, const char* name, at::ScalarType type, at::IntArrayRef sizes) const {
+        return o == Py_None ? nullptr : dense(o, name, type, sizes);
+    }
+    float* floats(PyObject* o, const char* name, at::IntArrayRef sizes) const { return static_cast<float*>(dense(o, name, at::kFloat, sizes)); }
+    float* floats_or_null(PyObject* o, const char* name, at::IntArrayRef sizes) const { return static_cast<float*>(dense_or_null(o, name, at::kFloat, sizes)); }
+    at::Tensor make(at::IntArrayRef sizes, at::ScalarType type) const { return at::empty(sizes, at::TensorOptions().dtype(type).device(dev)); }
+    void* stream() const { return c10::hip::getCurrentHIPStream(dev.index()).stream(); }
+};
+
+// A row output: the caller's tensor, checked, or a new one.
+struct RowsOut {
+    PyObject* o;                          // owned
+    Rows r;
+    RowsOut(const Seq& q, PyObject* given, const char* name) {
+        if (given != nullptr && given != Py_None) {
+            r = q.like(given, name);
+            o = given;
+            Py_INCREF(o);
+        } else {
+            at::Tensor v = q.make(q.shape, q.t);
+            r = Rows(v, name);
+            o = THPVariable_Wrap(std::move(v));
+            if (o == nullptr) throw Raised{};
+        }
+    }
+    RowsOut(const RowsOut&) = delete;
+    ~RowsOut() { Py_XDECREF(o); }
+    PyObject* release() { PyObject* v = o; o = nullptr; return v; }
+};
+// A dense output that may not exist.
+struct DenseOut {
+    PyObject* o = nullptr;                // owned
+    void* p = nullptr;
+    DenseOut(const Seq& q, bool exists, at::IntArrayRef sizes, at::ScalarType type = at::kFloat) {
+        if (!exists) {
+            o = Py_None;
+            Py_INCREF(o);
+            return;
+        }
+        at::Tensor v = q.make(sizes, type);
+        p = v.data_ptr();
+        o = THPVariable_Wrap(std::move(v));
+        if (o == nullptr) throw Raised{};
+    }
+    DenseOut(const DenseOut&) = delete;
+    ~DenseOut() { Py_XDECREF(o); }
+    float* f() const { return static_cast<float*>(p); }
+    PyObject* release() { PyObject* v = o; o = nullptr; return v; }
+};
+// The caller's buffer as it is, or a new one of this size.
+struct Buffer {
+    at::Tensor own;
+    void* p = nullptr;
+    size_t bytes = 0;
+    Buffer(const Seq& q, PyObject* o, const char* name, size_t size) {
+        if (o != Py_None) {
+            const at::Tensor& v = q.here(o, name);
+            if (!v.is_contiguous()) raise(PyExc_ValueError, std::string(name) + " must be contiguous");
+            p = v.data_ptr();
+            bytes = (size_t)v.numel() * v.element_size();
+        } else if (size > 0) {
+            own = q.make({(int64_t)size}, at::kByte);
+            p = own.data_ptr();
+            bytes = size;
+        }
+    }
+};
+
+double double_of(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) throw Raised{};
+    return v;
+}
+bool truth_of(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v != 0;
+}
+
+// The rows, gates and sequences that the calls of the recurrence share.
+struct Recur {
+    Seq q;
+    Rows x, r, i;
+    int64_t S;
+    float* lam;
+    int32_t *offsets, *lengths;
+    float* h0;
+    scan2d_recur_desc d = {};
+    Recur(PyObject* ox, PyObject* orr, PyObject* oi, PyObject* olam, PyObject* ooff, PyObject* olen, PyObject* oh0, PyObject* oscale, bool step = false)
+        : q(ox, "x", 2), x(q.like(ox, "x")), r(q.like(orr, "r")), i(q.like(oi, "i")) {
+        if (q.shape.size() > (step ? 2u : 3u)) raise(PyExc_ValueError, step ? "x: expected 2 dimensions" : "x: expected 2 or 3 dimensions");
+        lam = q.floats(olam, "lam", {q.C});
+        S = q.shape.size() == 3 ? q.shape[0] : 1;
+        offsets = lengths = nullptr;
+        if (ooff != Py_None) {
+            const at::Tensor& v = q.here(ooff, "offsets");
+            if (q.shape.size() != 2 || v.dim() != 1 || v.size(0) < 2) raise(PyExc_ValueError, "offsets: expected one dimension of at least 2 entries, and x of 2 dimensions");
+            S = v.size(0) - 1;
+            offsets = static_cast<int32_t*>(q.dense(ooff, "offsets", at::kInt, {S + 1}));
+        }
+        if (olen != Py_None) {
+            if (q.shape.size() != 3) raise(PyExc_ValueError, "lengths: expected x of 3 dimensions");
+            lengths = static_cast<int32_t*>(q.dense(olen, "lengths", at::kInt, {S}));
+        }
+        if (S > 0x7fffffff || S < 1) raise(PyExc_ValueError, "x: number of sequences out of range");
+        h0 = q.floats_or_null(oh0, "h0", {S, q.C});
+        d.T = q.rows; d.C = (int32_t)q.C; d.S = (int32_t)S;
+        d.dtype = q.t == at::kBFloat16 ? SCAN2D_BF16 : SCAN2D_F32;
+        d.scale = (float)double_of(oscale);
+        d.stride_x = x.stride; d.stride_r = r.stride; d.stride_i = i.stride;
+    }
+};
+
+PyObject* seq_recur_fwd(Args a) {         // x, r, i, lam, offsets, lengths, h0, scale, want_final, want_saved, h, workspace
+    Recur c(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]);
+    RowsOut h(c.q, a[10], "h");
+    c.d.stride_h = h.r.stride;
+    const size_t saved_bytes = scan2d_seq_recur_saved_bytes(&c.d);
+    const bool want = truth_of(a[9]);
+    DenseOut hT(c.q, truth_of(a[8]), {c.S, c.q.C}), saved(c.q, want, {(int64_t)saved_bytes}, at::kByte);
+    const Buffer w(c.q, a[11], "workspace", scan2d_seq_recur_workspace_bytes(&c.d, SCAN2D_PASS_FWD));
+    check_rc(unlocked(scan2d_seq_recur_fwd, &c.d, c.x.p, c.r.p, c.i.p, c.lam, c.offsets, c.lengths, c.h0, h.r.p, hT.f(), saved.p, want ? saved_bytes : 0,
+                      w.p, w.bytes, c.q.stream()), "scan2d_seq_recur_fwd");
+    return tuple(h, hT, saved);
+}
+
+PyObject* seq_recur_bwd(Args a) {         // x, r, i, lam, dh, saved, offsets, lengths, h0, dhT, scale, want_dh0, out, workspace
+    Recur c(a[0], a[1], a[2], a[3], a[6], a[7], a[8], a[10]);
+    const Rows dh = c.q.like(a[4], "dh");
+    const float* dhT = c.q.floats_or_null(a[9], "dhT", {c.S, c.q.C});
+    Given given;
+    if (a[12] != Py_None) given.unpack(a[12], 3, "out: expected three tensors");
+    RowsOut dx(c.q, given[0], "dx"), dr(c.q, given[1], "dr"), di(c.q, given[2], "di");
+    c.d.stride_dh = dh.stride; c.d.stride_dx = dx.r.stride; c.d.stride_dr = dr.r.stride; c.d.stride_di = di.r.stride;
+    if (a[5] == Py_None) raise(PyExc_ValueError, "saved is required");
+    const Buffer saved(c.q, a[5], "saved", 0);
+    DenseOut dlam(c.q, true, {c.q.C}), dh0(c.q, truth_of(a[11]), {c.S, c.q.C});
+    const Buffer w(c.q, a[13], "workspace", scan2d_seq_recur_workspace_bytes(&c.d, SCAN2D_PASS_BWD));
+    check_rc(unlocked(scan2d_seq_recur_bwd, &c.d, c.x.p, c.r.p, c.i.p, c.lam, c.offsets, c.lengths, c.h0, dh.p, dhT, saved.p, saved.bytes, dx.r.p, dr.r.p,
+                      di.r.p, dlam.f(), dh0.f(), w.p, w.bytes, c.q.stream()), "scan2d_seq_recur_bwd");
+    return tuple(dx, dr, di, dlam, dh0);
+}
+
+PyObject* seq_recur_step(Args a) {        // x, r, i, lam, state, slots, scale, h
+    Recur c(a[0], a[1], a[2], a[3], Py_None, Py_None, Py_None, a[6], true);
+    const at::Tensor& st = c.q.here(a[4], "state");
+    if (st.dim() != 2) raise(PyExc_ValueError, "state: expected 2 dimensions");
+    const int64_t n = st.size(0);
+    float* state = c.q.floats(a[4], "state", {n, c.q.C});
+    const int32_t* slots = static_cast<int32_t*>(c.q.dense_or_null(a[5], "slots", at::kInt, {c.q.rows}));
+    RowsOut h(c.q, a[7], "h");
+    c.d.stride_h = h.r.stride;
+    check_rc(unlocked(scan2d_seq_recur_step, &c.d, c.x.p, c.r.p, c.i.p, c.lam, state, slots, n, h.r.p, c.q.stream()), "scan2d_seq_recur_step");
+    return h.release();
+}
+
+struct GroupNorm {
+    Seq q;
+    Rows x;
+    float *gamma, *beta;
+    uint8_t* mask;
+    scan2d_group_norm_desc d = {};
+    GroupNorm(PyObject* ox, PyObject* og, PyObject* ob, PyObject* ogroups, PyObject* oeps, PyObject* oact, PyObject* om) : q(ox, "x", 3), x(q.like(ox, "x")) {
+        gamma = q.floats_or_null(og, "gamma", {q.C});
+        beta = q.floats_or_null(ob, "beta", {q.C});
+        mask = static_cast<uint8_t*>(q.dense_or_null(om, "mask", at::kByte, at::IntArrayRef(q.shape.data(), q.shape.size() - 1)));
+        const int64_t G = int_of(ogroups), act = int_of(oact);
+        if (q.rows < 1) raise(PyExc_ValueError, "x has no positions");
+        if (q.shape[0] > 0x7fffffff || G < 1 || G > q.C) raise(PyExc_ValueError, "groups: expected a divisor of the channels");
+        d.N = (int32_t)q.shape[0]; d.C = (int32_t)q.C; d.G = (int32_t)G; d.P = q.rows / q.shape[0];
+        d.dtype = q.t == at::kBFloat16 ? SCAN2D_BF16 : SCAN2D_F32;
+        d.act = act < 0 || act > 0x7fffffff ? -1 : (int32_t)act;
+        d.eps = oeps == nullptr ? 0.0f : (float)double_of(oeps);
+        d.stride_x = x.stride;
+    }
+};
+
+PyObject* group_norm_fwd(Args a) {        // x, gamma, beta, groups, eps, act, mask, y, workspace
+    GroupNorm c(a[0], a[1], a[2], a[3], a[4], a[5], a[6]);
+    RowsOut y(c.q, a[7], "y");
+    c.d.stride_y = y.r.stride;
+    DenseOut stats(c.q, true, {(int64_t)c.d.N, (int64_t)c.d.G, 2});
+    const Buffer w(c.q, a[8], "workspace", scan2d_group_norm_workspace_bytes(&c.d, SCAN2D_PASS_FWD));
+    check_rc(unlocked(scan2d_group_norm_fwd, &c.d, c.x.p, c.gamma, c.beta, c.mask, y.r.p, stats.f(), w.p, w.bytes, c.q.stream()), "scan2d_group_norm_fwd");
+    return tuple(y, stats);
+}
+
+PyObject* group_norm_bwd(Args a) {        // x, gamma, beta, groups, stats, dy, act, mask, dx, workspace
+    GroupNorm c(a[0], a[1], a[2], a[3], nullptr, a[6], a[7]);
+    const float* stats = c.q.floats(a[4], "stats", {(int64_t)c.d.N, (int64_t)c.d.G, 2});
+    const Rows dy = c.q.like(a[5], "dy");
+    RowsOut dx(c.q, a[8], "dx");
+    c.d.stride_dy = dy.stride; c.d.stride_dx = dx.r.stride;
+    DenseOut dgamma(c.q, c.gamma != nullptr, {c.q.C}), dbeta(c.q, c.beta != nullptr, {c.q.C});
+    const Buffer w(c.q, a[9], "workspace", scan2d_group_norm_workspace_bytes(&c.d, SCAN2D_PASS_BWD));
+    check_rc(unlocked(scan2d_group_norm_bwd, &c.d, c.x.p, c.gamma, c.beta, c.mask, stats, dy.p, dx.r.p, dgamma.f(), dbeta.f(), w.p, w.bytes, c.q.stream()),
+             "scan2d_group_norm_bwd");
+    return tuple(dx, dgamma, dbeta);
+}
+
 // ---- an entry point with its arguments converted once: call(address, arguments) enqueues it again on the current
 // stream, which is the last argument of every entry point.  Arguments are pointers and sizes, one 64-bit register or
 // stack slot each in this platform's C calling convention.
@@ -470,6 +736,11 @@ PyMethodDef methods[] = {
     SCAN2D_ENTRY("block_linear", block_linear, 5),
     SCAN2D_ENTRY("block_norm", block_norm, 6),
     SCAN2D_ENTRY("block_attn_pool", block_attn_pool, 5),
+    SCAN2D_ENTRY("seq_recur_fwd", seq_recur_fwd, 12),
+    SCAN2D_ENTRY("seq_recur_bwd", seq_recur_bwd, 14),
+    SCAN2D_ENTRY("seq_recur_step", seq_recur_step, 8),
+    SCAN2D_ENTRY("group_norm_fwd", group_norm_fwd, 9),
+    SCAN2D_ENTRY("group_norm_bwd", group_norm_bwd, 10),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

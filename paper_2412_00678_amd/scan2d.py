@@ -26,6 +26,8 @@ EXPORTS = ("scan2d_fwd", "scan2d_fwd_softplus", "scan2d_fwd_softplus_gated", "sc
            "scan2d_version", "scan2d_debug_force_variant", "scan2d_bwd_static_scratch", "scan2d_fwd_variants", "scan2d_bwd_variants",
            "scan2d_block_conv_silu", "scan2d_block_xproj", "scan2d_saved_bytes", "scan2d_fwd_saving", "scan2d_bwd_saved",
            "scan2d_block_attn_pool", "scan2d_block_linear", "scan2d_block_norm")
+SEQ_EXPORTS = ("scan2d_seq_recur_fwd", "scan2d_seq_recur_bwd", "scan2d_seq_recur_step", "scan2d_seq_recur_saved_bytes",
+               "scan2d_seq_recur_workspace_bytes", "scan2d_group_norm_fwd", "scan2d_group_norm_bwd", "scan2d_group_norm_workspace_bytes")
 STATIC_SCRATCH_BYTES = 32 * 1024 * 1024
 ERR_SCRATCH_LIMIT = -9
 TUNE_FWD, TUNE_FWD_SHARED, TUNE_BWD = 0, 1, 2
@@ -43,6 +45,16 @@ class Variants(ctypes.Structure):
 
 class ConvShape(ctypes.Structure):
     _fields_ = [("KH", ctypes.c_int32), ("KW", ctypes.c_int32), ("PH", ctypes.c_int32), ("PW", ctypes.c_int32)]
+
+
+class RecurDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("C", ctypes.c_int32), ("S", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                *((f"stride_{k}", ctypes.c_int64) for k in ("x", "r", "i", "h", "dh", "dx", "dr", "di"))]
+
+
+class GroupNormDesc(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("C", ctypes.c_int32), ("G", ctypes.c_int32), ("P", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("eps", ctypes.c_float), *((f"stride_{k}", ctypes.c_int64) for k in ("x", "y", "dy", "dx"))]
 
 
 class Scan2dError(RuntimeError):
@@ -101,6 +113,19 @@ def _load() -> ctypes.CDLL:
     lib.scan2d_describe_plan.restype = ctypes.c_int
     lib.scan2d_debug_force_variant.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_int), ctypes.c_int]
     lib.scan2d_debug_force_variant.restype = ctypes.c_int
+    lib.scan2d_seq_recur_fwd.argtypes = [ctypes.POINTER(RecurDesc)] + [vp] * 10 + [ctypes.c_size_t, vp, ctypes.c_size_t, vp]
+    lib.scan2d_seq_recur_bwd.argtypes = [ctypes.POINTER(RecurDesc)] + [vp] * 10 + [ctypes.c_size_t] + [vp] * 6 + [ctypes.c_size_t, vp]
+    lib.scan2d_seq_recur_step.argtypes = [ctypes.POINTER(RecurDesc)] + [vp] * 6 + [ctypes.c_int64, vp, vp]
+    lib.scan2d_group_norm_fwd.argtypes = [ctypes.POINTER(GroupNormDesc)] + [vp] * 7 + [ctypes.c_size_t, vp]
+    lib.scan2d_group_norm_bwd.argtypes = [ctypes.POINTER(GroupNormDesc)] + [vp] * 10 + [ctypes.c_size_t, vp]
+    for fn in (lib.scan2d_seq_recur_fwd, lib.scan2d_seq_recur_bwd, lib.scan2d_seq_recur_step, lib.scan2d_group_norm_fwd, lib.scan2d_group_norm_bwd):
+        fn.restype = ctypes.c_int
+    lib.scan2d_seq_recur_saved_bytes.argtypes = [ctypes.POINTER(RecurDesc)]
+    lib.scan2d_seq_recur_saved_bytes.restype = ctypes.c_size_t
+    lib.scan2d_seq_recur_workspace_bytes.argtypes = [ctypes.POINTER(RecurDesc), ctypes.c_int]
+    lib.scan2d_seq_recur_workspace_bytes.restype = ctypes.c_size_t
+    lib.scan2d_group_norm_workspace_bytes.argtypes = [ctypes.POINTER(GroupNormDesc), ctypes.c_int]
+    lib.scan2d_group_norm_workspace_bytes.restype = ctypes.c_size_t
     return lib
 
 
@@ -419,6 +444,45 @@ def block_attn_pool(h, V, w, mask=None, out=None):
     """(z [Bt][M] fp32, attn [Bt][H][W] fp32) from h [Bt][M][H][W], V [D][M] (type of h), w [D] fp32 and an optional
     mask [Bt][H][W] uint8 (non-zero = not in the bag)."""
     return _native.block_attn_pool(h, V, w, mask, out)
+
+
+def seq_recur_fwd(x, r, i, lam, offsets=None, lengths=None, h0=None, scale=8.0, want_final=False, want_saved=False, h=None, workspace=None):
+    """The gated linear recurrence over token sequences, channels last: (h, hT or None, saved or None) with
+
+        a = exp(-scale * softplus(lam) * sigmoid(r)),    h_t = a * h_{t-1} + sqrt(1 - a^2) * sigmoid(i) * x
+
+    x, r, i: [T][C] (one sequence, or with offsets [S + 1] int32 on the device S packed ones; rows behind the last are left
+    as they are) or [S][L][C] (S sequences of L tokens, or with lengths [S] int32 on the device of so many), fp32 or bf16, each with rows
+    at a stride of its own; lam: [C] fp32; h0: [S][C] fp32, the states before the first tokens (None: zero).
+    hT: [S][C] fp32, the states behind the last ones; saved: what seq_recur_bwd needs of the states; h: a tensor to write into."""
+    return _native.seq_recur_fwd(x, r, i, lam, offsets, lengths, h0, scale, want_final, want_saved, h, workspace)
+
+
+def seq_recur_bwd(x, r, i, lam, dh, saved, offsets=None, lengths=None, h0=None, dhT=None, scale=8.0, want_dh0=None, out=None, workspace=None):
+    """Gradients (dx, dr, di, dlam, dh0 or None) of sum(dh * h) + sum(dhT * hT) for the arguments that seq_recur_fwd had
+    and what it saved.  want_dh0: by default where h0 is given.  out: (dx, dr, di), tensors to write into or None each."""
+    return _native.seq_recur_bwd(x, r, i, lam, dh, saved, offsets, lengths, h0, dhT, scale, h0 is not None if want_dh0 is None else want_dh0, out, workspace)
+
+
+def seq_recur_step(x, r, i, lam, state, slots=None, scale=8.0, h=None):
+    """One token for each of T sequences: h [T][C] of x, r, i [T][C]; state [slot count][C] fp32 is replaced in place.  Row t
+    has the state slots[t] (int32, device; None: t); a row with a slot out of range is padding and its h is left as it is."""
+    return _native.seq_recur_step(x, r, i, lam, state, slots, scale, h)
+
+
+ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
+
+
+def group_norm_fwd(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, mask=None, y=None, workspace=None):
+    """(y, stats) with y = act(group norm of x * gamma + beta), channels last: x [N][...][C], any number of position
+    dimensions between (at least one), fp32 or bf16; gamma, beta: [C] fp32 or None; mask [N][...] uint8 (non-zero: the position counts for
+    nothing and its y is 0).  stats: [N][groups][2] fp32, for group_norm_bwd.  y: a tensor to write into, x itself for in place."""
+    return _native.group_norm_fwd(x, gamma, beta, groups, eps, act, mask, y, workspace)
+
+
+def group_norm_bwd(x, gamma, beta, groups, stats, dy, act=ACT_NONE, mask=None, dx=None, workspace=None):
+    """Gradients (dx, dgamma, dbeta) of sum(dy * y); dgamma / dbeta are None where gamma / beta are."""
+    return _native.group_norm_bwd(x, gamma, beta, groups, stats, dy, act, mask, dx, workspace)
 
 
 def to_device(arrs: dict, dtype_code: int, device="cuda:0") -> dict:

@@ -1,0 +1,605 @@
+"""GPU parity of the sequence layers (scan2d_seq_recur_*, scan2d_group_norm_*) with oracle/seq.py, through the binding.
+
+Tolerances: the oracle's own element-wise bound for fp32 arithmetic, plus the one rounding to the storage type (at most
+half a step: 2^-8 of the value for bf16, 2^-24 for fp32)."""
+import numpy as np
+import pytest
+
+from oracle import seq
+
+pytestmark = pytest.mark.gpu
+
+HALF_STEP = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch
+
+
+@pytest.fixture(scope="module")
+def s2d(torch):
+    from paper_2412_00678_amd import scan2d          # raises if the library is not built
+    return scan2d
+
+
+def host(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def close(name, got, ref, dtype):
+    """|got - value| <= bound + half a step of the storage type."""
+    value, bound = ref
+    got = host(got).reshape(value.shape)
+    assert np.isfinite(got).all() == np.isfinite(value).all(), name
+    tol = bound + HALF_STEP[dtype] * (np.abs(value) + bound)
+    off = np.abs(got - value)
+    worst = np.unravel_index(np.argmax(off - tol), off.shape) if off.size else ()
+    assert (off <= tol).all(), f"{name} at {worst}: {got[worst]!r} for {value[worst]!r}, off {off[worst]:.3e} > {tol[worst]:.3e}"
+
+
+def rows(torch, rng, shape, dtype, scale=1.0, pad=None):
+    """Rows in the storage type; pad = (channels before, channels behind): a view into wider rows."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    lo, hi = pad or (0, 0)
+    wide = torch.from_numpy((rng.normal(size=(*shape[:-1], lo + shape[-1] + hi)) * scale).astype(np.float32)).to(dt).cuda()
+    return wide[..., lo:lo + shape[-1]]
+
+
+def decays(rng, C):
+    """lam with softplus(lam) between 1e-4 and 1: decays from slow to fast."""
+    sp = np.exp(rng.uniform(np.log(1e-4), 0, C))
+    return np.log(np.expm1(sp)).astype(np.float32)
+
+
+def spans_of(layout, lens, L=0):
+    if layout == "packed":
+        ends = np.cumsum(lens)
+        return [(int(e - n), int(e)) for e, n in zip(ends, lens)]
+    return [(s * L, s * L + n) for s, n in enumerate(lens)]
+
+
+def recur_case(torch, s2d, layout, lens, L, C, dtype, seed, states=True, pad=None, behind=0, scale=8.0, gate=2.0):
+    """Forward, backward and both again: compared with the oracle, rows of no sequence untouched, the same bits twice."""
+    rng = np.random.default_rng(seed)
+    S = len(lens)
+    T = (sum(lens) if layout == "packed" else S * L) + behind
+    spans = spans_of(layout, lens, L)
+    shape = (T, C) if layout == "packed" else (S, L, C)
+    x, r, i, dh = (rows(torch, rng, shape, dtype, s, pad) for s in (1.0, gate, gate, 1.0))
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    h0, dhT = (torch.from_numpy(rng.normal(size=(S, C)).astype(np.float32)).cuda() if states else None for _ in range(2))
+    kw = dict(h0=h0, scale=scale)
+    if layout == "packed":
+        kw["offsets"] = torch.tensor([0, *np.cumsum(lens)], dtype=torch.int32, device="cuda")
+    elif layout == "padded":
+        kw["lengths"] = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    flat = lambda t: host(t).reshape(T, C)
+    ref = seq.recur(flat(x), flat(r), flat(i), host(lam), spans, None if h0 is None else host(h0), scale, flat(dh), None if dhT is None else host(dhT))
+    print(f"recurrence {layout} S={S} T={T} C={C} {dtype} pad={pad} behind={behind}", flush=True)
+
+    def once():
+        out = [torch.full((*shape[:-1], C + sum(pad or (0, 0))), 7.0, dtype=x.dtype, device="cuda") for _ in range(4)]
+        cut = [o[..., (pad or (0, 0))[0]:][..., :C] for o in out]
+        h, hT, saved = s2d.seq_recur_fwd(x, r, i, lam, want_final=True, want_saved=True, h=cut[0], **kw)
+        dx, dr, di, dlam, dh0 = s2d.seq_recur_bwd(x, r, i, lam, dh, saved, dhT=dhT, want_dh0=True, out=cut[1:], **kw)
+        torch.cuda.synchronize()
+        return dict(h=h, hT=hT, dx=dx, dr=dr, di=di, dlam=dlam, dh0=dh0), out
+
+    got, wide = once()
+    inside = np.zeros(T, bool)
+    for lo, hi in spans:
+        inside[lo:hi] = True
+    for name in ("h", "dx", "dr", "di"):
+        value, bound = ref[name]
+        t = got[name].reshape(T, C)
+        close(name, t[torch.from_numpy(inside).cuda()], (value[inside], bound[inside]), dtype)
+        assert (host(t)[~inside] == 7.0).all(), name                          # rows of no sequence
+    for o in wide:                                                            # and nothing beside the channels
+        if pad is not None:
+            flat_o = host(o).reshape(T, -1)
+            assert (flat_o[:, :pad[0]] == 7.0).all() and (flat_o[:, pad[0] + C:] == 7.0).all()
+    for name in ("hT", "dlam", "dh0"):
+        close(name, got[name], ref[name], "fp32")
+    again, _ = once()
+    for name in got:
+        assert torch.equal(got[name], again[name]), name
+    return got
+
+
+RECUR_CASES = [
+    # layout, lengths, rows per sequence, channels, dtype, options
+    ("packed", [1], 0, 1, "fp32", {}),
+    ("packed", [1], 0, 64, "bf16", {"states": False}),
+    ("packed", [2, 1], 0, 2, "bf16", {}),
+    ("packed", [0], 0, 5, "fp32", {}),
+    ("packed", [0, 5, 0, 0, 1, 131, 0], 0, 3, "fp32", {}),
+    ("packed", [0, 0, 37, 0], 0, 65, "bf16", {"behind": 90}),
+    ("packed", [64], 0, 64, "fp32", {}),
+    ("packed", [65, 63, 1, 127, 128, 129], 0, 127, "bf16", {}),
+    ("packed", [257], 0, 128, "bf16", {}),
+    ("packed", [300, 0, 17], 0, 129, "fp32", {"behind": 3}),
+    ("packed", [700], 0, 130, "bf16", {"pad": (1, 2)}),
+    ("packed", [100, 411], 0, 33, "fp32", {"pad": (3, 0)}),
+    ("packed", [1] * 300, 0, 40, "bf16", {}),
+    ("packed", [3, 1, 2, 0, 4] * 60, 0, 31, "fp32", {}),
+    ("packed", [2500], 0, 31, "bf16", {}),
+    ("packed", [1700, 900], 0, 257, "fp32", {"states": False}),
+    ("packed", [4000], 0, 8, "fp32", {"scale": 0.5}),
+    ("padded", [0, 7, 50, 1], 50, 66, "bf16", {}),
+    ("padded", [200, 0, 0, 129], 200, 24, "fp32", {"pad": (0, 24)}),
+    ("padded", [0, 0], 3, 4, "bf16", {}),
+    ("equal", [100] * 3, 100, 70, "bf16", {}),
+    ("equal", [1] * 5, 1, 256, "fp32", {}),
+    ("equal", [1000] * 2, 1000, 96, "fp32", {"gate": 8.0}),
+]
+
+
+@pytest.mark.parametrize("case", RECUR_CASES, ids=lambda c: f"{c[0]}-{len(c[1])}x{sum(c[1])}-C{c[3]}-{c[4]}" + "".join(f"-{k}" for k in c[5]))
+def test_recurrence_matches_the_oracle(torch, s2d, case):
+    layout, lens, L, C, dtype, options = case
+    recur_case(torch, s2d, layout, lens, L, C, dtype, seed=sum(lens) + C, **options)
+
+
+def test_recurrence_random_shapes_match_the_oracle(torch, s2d):
+    rng = np.random.default_rng(99)
+    for k in range(12):
+        layout = ("packed", "padded", "equal")[k % 3]
+        S, L = int(rng.integers(1, 9)), int(np.exp(rng.uniform(0, np.log(500))))
+        lens = [L] * S if layout == "equal" else [int(n) for n in rng.integers(0, L + 1, S)]
+        recur_case(torch, s2d, layout, lens, L, int(np.exp(rng.uniform(0, np.log(400)))), ("fp32", "bf16")[int(rng.integers(2))], seed=k,
+                   behind=int(rng.integers(0, 40)) if layout == "packed" else 0)
+
+
+def test_recurrence_of_no_rows(torch, s2d):
+    x = torch.empty((0, 6), device="cuda")
+    lam = torch.zeros(6, device="cuda")
+    h0, dhT = torch.randn(2, 6, device="cuda"), torch.randn(2, 6, device="cuda")
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    h, hT, saved = s2d.seq_recur_fwd(x, x, x, lam, offsets=off, h0=h0, want_final=True, want_saved=True)
+    dx, dr, di, dlam, dh0 = s2d.seq_recur_bwd(x, x, x, lam, x, saved, offsets=off, h0=h0, dhT=dhT)
+    torch.cuda.synchronize()
+    assert h.shape == (0, 6) and torch.equal(hT, h0) and torch.equal(dh0, dhT) and bool((dlam == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_recurrence_at_the_ends_of_the_gates(torch, s2d, dtype):
+    """Gates that are shut or open to the last bit, decays of exactly 1 and 0, and the gradients through them."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    vals = [-1e30, -200.0, -88.0, -30.0, 0.0, 30.0, 88.0, 200.0, 1e30]
+    r = torch.tensor(vals * 8, device="cuda").to(dt)[:, None].expand(72, 7).contiguous()
+    i = torch.tensor([v for v in vals for _ in range(8)], device="cuda").to(dt)[:, None].expand(72, 7).contiguous()
+    rng = np.random.default_rng(3)
+    x, dh = rows(torch, rng, (72, 7), dtype), rows(torch, rng, (72, 7), dtype)
+    lam = torch.tensor([-100.0, -40.0, -16.0, -5.0, 0.0, 19.0, 60.0], device="cuda")
+    h0 = torch.ones(1, 7, device="cuda")
+    h, hT, saved = s2d.seq_recur_fwd(x, r, i, lam, h0=h0, want_final=True, want_saved=True)
+    dx, dr, di, dlam, dh0 = s2d.seq_recur_bwd(x, r, i, lam, dh, saved, h0=h0)
+    torch.cuda.synchronize()
+    ref = seq.recur(host(x), host(r), host(i), host(lam), [(0, 72)], host(h0), 8.0, host(dh))
+    for name, t in dict(h=h, dx=dx, dr=dr, di=di).items():
+        close(name, t, ref[name], dtype)
+    for name, t in dict(hT=hT, dlam=dlam, dh0=dh0).items():
+        close(name, t, ref[name], "fp32")
+
+
+def test_recurrence_nan_stays_in_its_sequence_and_channel(torch, s2d):
+    rng = np.random.default_rng(5)
+    x, r, i = (rows(torch, rng, (600, 70), "fp32") for _ in range(3))
+    off = torch.tensor([0, 200, 420, 600], dtype=torch.int32, device="cuda")
+    lam = torch.from_numpy(decays(rng, 70)).cuda()
+    clean, cT, _ = s2d.seq_recur_fwd(x, r, i, lam, offsets=off, want_final=True)
+    x[250, 9], i[300, 30] = float("nan"), float("inf")                        # an open gate is no NaN
+    h, hT, saved = s2d.seq_recur_fwd(x, r, i, lam, offsets=off, want_final=True, want_saved=True)
+    torch.cuda.synchronize()
+    bad = torch.isnan(h)
+    want = torch.zeros_like(bad)
+    want[250:420, 9] = True
+    assert torch.equal(bad, want) and torch.equal(torch.isnan(hT), want[[199, 419, 599]])
+    keep = ~want
+    keep[300:420, 30] = False
+    assert torch.equal(h[keep], clean[keep])
+
+
+def test_recurrence_in_pieces_is_the_whole(torch, s2d):
+    """A prompt in pieces, each from the state that the one before left, then token by token."""
+    rng = np.random.default_rng(11)
+    T, C = 700, 96
+    x, r, i = (rows(torch, rng, (T, C), "bf16") for _ in range(3))
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    ref = seq.recur(host(x), host(r), host(i), host(lam), [(0, T)])
+    state = torch.zeros(1, C, device="cuda")
+    parts = []
+    for lo, hi in ((0, 1), (1, 300), (300, 430), (430, 690)):
+        h, state, _ = s2d.seq_recur_fwd(x[lo:hi], r[lo:hi], i[lo:hi], lam, h0=state, want_final=True)
+        parts.append(h)
+    for t in range(690, T):
+        parts.append(s2d.seq_recur_step(x[t:t + 1], r[t:t + 1], i[t:t + 1], lam, state))
+    torch.cuda.synchronize()
+    close("h", torch.cat(parts), ref["h"], "bf16")
+    close("hT", state, ref["hT"], "fp32")
+
+
+@pytest.mark.parametrize("T,C,dtype,pad", [(1, 1, "fp32", None), (3, 2, "bf16", None), (4, 257, "bf16", (1, 0)), (65, 130, "fp32", (0, 130)),
+                                           (300, 64, "bf16", None), (2, 1000, "bf16", None), (1025, 7, "fp32", None)])
+def test_step_matches_the_oracle(torch, s2d, T, C, dtype, pad):
+    rng = np.random.default_rng(T + C)
+    x, r, i = (rows(torch, rng, (T, C), dtype, s, pad) for s in (1.0, 2.0, 2.0))
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    pool = torch.from_numpy(rng.normal(size=(2 * T + 1, C)).astype(np.float32)).cuda()
+    slots = rng.permutation(2 * T + 1)[:T].astype(np.int32)
+    if T > 3:
+        slots[1], slots[T // 2], slots[T - 1] = -1, 2 * T + 1, -2 ** 31              # padding
+    live = [(t, int(s)) for t, s in enumerate(slots) if 0 <= s <= 2 * T]
+    for dev in (torch.from_numpy(slots).cuda(), None):
+        state = pool.clone()
+        order = live if dev is not None else [(t, t) for t in range(T)]
+        h = torch.full((T, C), 7.0, dtype=x.dtype, device="cuda")
+        s2d.seq_recur_step(x, r, i, lam, state, slots=dev, h=h)
+        torch.cuda.synchronize()
+        at, to = [t for t, _ in order], [s for _, s in order]
+        ref = seq.recur(host(x)[at], host(r)[at], host(i)[at], host(lam), [(k, k + 1) for k in range(len(at))], host(pool)[to])
+        close("h", h[at], ref["h"], dtype)
+        close("state", state[to], ref["hT"], "fp32")
+        rest = [s for s in range(2 * T + 1) if s not in set(to)]
+        assert torch.equal(state[rest], pool[rest])
+        skipped = [t for t in range(T) if t not in set(at)]
+        assert bool((h[skipped] == 7.0).all())
+
+
+def test_step_takes_a_repeated_slot_in_the_order_of_its_rows(torch, s2d):
+    rng = np.random.default_rng(21)
+    T, C = 400, 129
+    x, r, i = (rows(torch, rng, (T, C), "fp32") for _ in range(3))
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    slots = torch.from_numpy(rng.integers(-1, 6, T).astype(np.int32)).cuda()
+    pool = torch.from_numpy(rng.normal(size=(6, C)).astype(np.float32)).cuda()
+    state, h = pool.clone(), torch.full((T, C), 7.0, device="cuda")
+    s2d.seq_recur_step(x, r, i, lam, state, slots=slots, h=h)
+    one, each = pool.clone(), torch.full((T, C), 7.0, device="cuda")
+    for t in range(T):
+        s2d.seq_recur_step(x[t:t + 1], r[t:t + 1], i[t:t + 1], lam, one, slots=slots[t:t + 1], h=each[t:t + 1])
+    torch.cuda.synchronize()
+    assert torch.equal(state, one) and torch.equal(h, each)
+
+
+def test_recurrence_bad_offsets_stay_inside(torch, s2d):
+    """Offsets and lengths outside the documented rules: any result, but nothing beside the tensors is touched."""
+    rng = np.random.default_rng(31)
+    T, C = 300, 66
+    buf = torch.full((3 * T, C), 7.0, device="cuda")
+    x, r, i, dh = (rows(torch, rng, (T, C), "fp32") for _ in range(4))
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    for off in ([0, 1000, 300], [-5, 100, 300], [0, 200, 100], [2 ** 31 - 1, -2 ** 31, 7], [300, 0, 0]):
+        o = torch.tensor(off, dtype=torch.int32, device="cuda")
+        h0 = torch.zeros(2, C, device="cuda")
+        _, _, saved = s2d.seq_recur_fwd(x, r, i, lam, offsets=o, h0=h0, want_final=True, want_saved=True, h=buf[T:2 * T])
+        s2d.seq_recur_bwd(x, r, i, lam, dh, saved, offsets=o, h0=h0, out=(buf[T:2 * T], None, None))
+        torch.cuda.synchronize()
+        assert bool((buf[:T] == 7.0).all()) and bool((buf[2 * T:] == 7.0).all())
+    x3, lens = x.reshape(3, 100, C), torch.tensor([-4, 1000, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    h, hT, saved = s2d.seq_recur_fwd(x3, r.reshape(3, 100, C), i.reshape(3, 100, C), lam, lengths=lens, want_final=True, want_saved=True,
+                                     h=buf[T:2 * T].reshape(3, 100, C))
+    torch.cuda.synchronize()
+    assert bool((buf[:T] == 7.0).all()) and bool((buf[2 * T:] == 7.0).all()) and bool(torch.isfinite(hT).all())
+
+
+def test_recurrence_past_32_bit_offsets(torch, s2d):
+    """Rows whose offsets pass 2^31 elements: the last rows against the same rows by themselves."""
+    T, C = 2 ** 21 + 77, 1024
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty((T, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    lam = torch.zeros(C, device="cuda")                                        # scale 8: a state is forgotten within some tokens
+    h, hT, saved = s2d.seq_recur_fwd(x, x, x, lam, want_final=True, want_saved=True)
+    n = 2000
+    h2, hT2, saved2 = s2d.seq_recur_fwd(x[-n:], x[-n:], x[-n:], lam, want_final=True, want_saved=True)
+    torch.cuda.synchronize()
+    assert torch.equal(h[-n + 1000:], h2[1000:])
+    assert float((hT - hT2).abs().max()) <= 1e-5
+    dx, dr, di, dlam, _ = s2d.seq_recur_bwd(x, x, x, lam, x, saved)
+    dx2, dr2, di2, _, _ = s2d.seq_recur_bwd(x[-n:], x[-n:], x[-n:], lam, x[-n:], saved2)
+    torch.cuda.synchronize()
+    for a, b in ((dx, dx2), (dr, dr2), (di, di2)):
+        assert float((a[-n + 1000:].float() - b[1000:].float()).abs().max()) <= 2.0 ** -7 * float(b.float().abs().max())
+    assert bool(torch.isfinite(dlam).all())
+
+
+NORM_CASES = [
+    # N, P, C, G, dtype, act, mask, affine, options
+    (1, 1, 1, 1, "fp32", "none", False, True, {}),
+    (2, 1, 8, 2, "bf16", "silu", False, True, {}),
+    (5, 1, 64, 4, "fp32", "gelu", False, True, {}),
+    (37, 1, 257, 1, "bf16", "silu", False, True, {}),
+    (300, 1, 96, 96, "fp32", "none", False, True, {}),
+    (7, 1, 2048, 16, "bf16", "silu", False, False, {}),
+    (3, 1, 6000, 3, "fp32", "silu", False, True, {}),
+    (64, 1, 640, 5, "bf16", "gelu", True, True, {}),
+    (2, 3, 10, 5, "fp32", "gelu", False, True, {}),
+    (3, 49, 32, 32, "bf16", "silu", True, True, {}),
+    (2, 196, 96, 32, "fp32", "silu", False, True, {}),
+    (8, 196, 64, 8, "bf16", "none", False, True, {"pad": (1, 3)}),
+    (1, 1000, 36, 4, "bf16", "gelu", True, True, {}),
+    (2, 777, 33, 11, "fp32", "silu", True, False, {"pad": (0, 5)}),
+    (1, 5000, 130, 2, "bf16", "silu", True, True, {}),
+    (4, 300, 513, 27, "fp32", "none", True, True, {}),
+    (2, 4100, 24, 1, "bf16", "silu", False, True, {}),
+    (70, 20, 48, 6, "fp32", "gelu", True, True, {}),
+    (1, 9000, 7, 7, "fp32", "silu", True, True, {}),
+    (1, 20000, 64, 32, "fp32", "silu", True, True, {}),
+]
+
+
+def norm_case(torch, s2d, N, P, C, G, dtype, act, masked, affine, seed, pad=None, eps=1e-5):
+    rng = np.random.default_rng(seed)
+    x, dy = rows(torch, rng, (N, P, C), dtype, 1.5, pad), rows(torch, rng, (N, P, C), dtype, 1.0, pad)
+    gamma, beta = (torch.from_numpy(v.astype(np.float32)).cuda() if affine else None
+                   for v in (rng.normal(size=C) * 0.3 + 1, rng.normal(size=C) * 0.3))
+    mask = None
+    if masked:
+        mask = (rng.random((N, P)) < 0.4).astype(np.uint8) * 3
+        mask[N // 2] = 1                                                       # an item of no positions
+        if N > 1:
+            mask[0, :] = 1
+            mask[0, P // 2] = 0                                                # and one of a single one
+        x[torch.from_numpy(mask).cuda() != 0] = float("nan")
+        dy[torch.from_numpy(mask).cuda() != 0] = float("inf")
+        mask = torch.from_numpy(mask).cuda()
+    code = {"none": s2d.ACT_NONE, "silu": s2d.ACT_SILU, "gelu": s2d.ACT_GELU}[act]
+    param = lambda t: None if t is None else host(t)
+    print(f"group norm N={N} P={P} C={C} G={G} {dtype} {act} masked={masked} affine={affine} pad={pad}", flush=True)
+    ref = seq.group_norm(host(x), param(gamma), param(beta), G, eps, act, None if mask is None else mask.cpu().numpy(), host(dy))
+
+    def once():
+        out = [torch.full((N, P, C + sum(pad or (0, 0))), 7.0, dtype=x.dtype, device="cuda") for _ in range(2)]
+        cut = [o[..., (pad or (0, 0))[0]:][..., :C] for o in out]
+        y, stats = s2d.group_norm_fwd(x, gamma, beta, G, eps=eps, act=code, mask=mask, y=cut[0])
+        dx, dgamma, dbeta = s2d.group_norm_bwd(x, gamma, beta, G, stats, dy, act=code, mask=mask, dx=cut[1])
+        torch.cuda.synchronize()
+        return dict(y=y, stats=stats, dx=dx, dgamma=dgamma, dbeta=dbeta), out
+
+    got, wide = once()
+    for name in ("y", "dx"):
+        close(name, got[name], ref[name], dtype)
+    close("stats", got["stats"], ref["stats"], "fp32")
+    for name in ("dgamma", "dbeta"):
+        if affine:
+            close(name, got[name], ref[name], "fp32")
+        else:
+            assert got[name] is None
+    if pad is not None:
+        for o in wide:
+            assert bool((o[..., :pad[0]] == 7.0).all()) and bool((o[..., pad[0] + C:] == 7.0).all())
+    if masked:
+        out = mask != 0
+        assert bool((got["y"][out] == 0).all()) and bool((got["dx"][out] == 0).all())
+    again, _ = once()
+    for name in got:
+        assert got[name] is None or torch.equal(got[name], again[name]), name
+    return got
+
+
+@pytest.mark.parametrize("case", NORM_CASES, ids=lambda c: "x".join(map(str, c[:4])) + f"-{c[4]}-{c[5]}" + ("-mask" if c[6] else "") + ("" if c[7] else "-plain"))
+def test_group_norm_matches_the_oracle(torch, s2d, case):
+    N, P, C, G, dtype, act, masked, affine, options = case
+    norm_case(torch, s2d, N, P, C, G, dtype, act, masked, affine, seed=N + P + C, **options)
+
+
+def test_group_norm_random_shapes_match_the_oracle(torch, s2d):
+    rng = np.random.default_rng(7)
+    for k in range(16):
+        G = int(rng.choice([1, 2, 3, 4, 8, 16, 32]))
+        C = G * int(np.exp(rng.uniform(0, np.log(600 // G))))
+        N, P = int(np.exp(rng.uniform(0, np.log(40)))), int(np.exp(rng.uniform(0, np.log(3000))))
+        P = max(1, min(P, 600000 // (N * C)))
+        norm_case(torch, s2d, N, P, C, G, ("fp32", "bf16")[k % 2], ("none", "silu", "gelu")[k % 3], bool(rng.integers(2)), bool(rng.integers(4)), seed=k)
+
+
+@pytest.mark.parametrize("P", [5, 4000])
+def test_group_norm_of_a_large_mean_keeps_its_variance(torch, s2d, P):
+    """Values around 1000 with a spread of 1: the squares are those of the deviations."""
+    rng = np.random.default_rng(13)
+    x = torch.from_numpy((1000 + rng.normal(size=(2, P, 64))).astype(np.float32)).cuda()
+    y, stats = s2d.group_norm_fwd(x, None, None, 4)
+    torch.cuda.synchronize()
+    ref = seq.group_norm(host(x), None, None, 4, 1e-5)
+    close("y", y, ref["y"], "fp32")
+    assert float(np.abs(host(y) - ref["y"][0]).max()) < 2e-3                    # 2^-24 of 1000 on the mean, 6e-5, and some sums
+
+
+def test_group_norm_in_place(torch, s2d):
+    rng = np.random.default_rng(17)
+    for shape in ((3, 50, 40), (1, 9000, 40), (50, 1, 320)):
+        x, dy = rows(torch, rng, shape, "bf16"), rows(torch, rng, shape, "bf16")
+        y, stats = s2d.group_norm_fwd(x, None, None, 4, act=s2d.ACT_SILU)
+        dx, _, _ = s2d.group_norm_bwd(x, None, None, 4, stats, dy, act=s2d.ACT_SILU)
+        x2, dy2 = x.clone(), dy.clone()
+        y2, _ = s2d.group_norm_fwd(x2, None, None, 4, act=s2d.ACT_SILU, y=x2)
+        dx2, _, _ = s2d.group_norm_bwd(x, None, None, 4, stats, dy2, act=s2d.ACT_SILU, dx=dy2)
+        torch.cuda.synchronize()
+        assert y2 is x2 and dx2 is dy2 and torch.equal(y, x2) and torch.equal(dx, dy2)
+
+
+def test_group_norm_of_maps_and_of_views(torch, s2d):
+    """[N][H][W][C] with a mask of its own dimensions; a channels-last image tensor by its permutation; a zero eps."""
+    rng = np.random.default_rng(19)
+    img = torch.from_numpy(rng.normal(size=(2, 24, 9, 11)).astype(np.float32)).cuda().contiguous(memory_format=torch.channels_last)
+    x = img.permute(0, 2, 3, 1)
+    mask = torch.from_numpy((rng.random((2, 9, 11)) < 0.3).astype(np.uint8)).cuda()
+    y, _ = s2d.group_norm_fwd(x, None, None, 6, mask=mask, eps=0.0)
+    torch.cuda.synchronize()
+    ref = seq.group_norm(host(x).reshape(2, 99, 24), None, None, 6, 0.0, mask=mask.cpu().numpy().reshape(2, 99))
+    close("y", y, ref["y"], "fp32")
+
+
+def test_group_norm_past_32_bit_offsets(torch, s2d):
+    N, P, C, G = 2, 2 ** 20 + 5, 1040, 4
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.empty((N, P, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    gamma, beta = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    y, stats = s2d.group_norm_fwd(x, gamma, beta, G)
+    torch.cuda.synchronize()
+    for n in range(N):
+        for k in range(G):
+            w = x[n, :, k * 260:(k + 1) * 260].float()
+            assert abs(float(stats[n, k, 0]) - float(w.double().mean())) < 1e-5
+            assert abs(float(stats[n, k, 1]) - 1.0) < 1e-3
+    last = x[1, -7:].float().reshape(7, G, 260)
+    want = ((last - stats[1, :, 0, None]) * stats[1, :, 1, None]).reshape(7, C)
+    assert float((y[1, -7:].float() - want).abs().max()) <= 2.0 ** -8 * float(want.abs().max()) + 1e-5
+    dx, dgamma, dbeta = s2d.group_norm_bwd(x, gamma, beta, G, stats, x)
+    torch.cuda.synchronize()
+    # dy = x: dv = x, so dx = rstd (x - mean x - xh mean(x xh)); with mean(x xh) = 1 / rstd (up to eps) that is about 0
+    assert float(dx[1, -1000:].float().abs().max()) < 1e-2
+    assert float((dbeta - x.float().sum((0, 1))).abs().max()) < 1.0
+
+
+def chain_inputs(torch, rng, T, C, dtype):
+    x, gates, dy = rows(torch, rng, (T, C), dtype), rows(torch, rng, (T, 2 * C), dtype), rows(torch, rng, (T, C), dtype)
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    gamma, beta = (torch.from_numpy((rng.normal(size=C) * 0.2 + m).astype(np.float32)).cuda() for m in (1.0, 0.0))
+    return x, gates, dy, lam, gamma, beta
+
+
+def chain(torch, s2d, x, gates, dy, lam, gamma, beta, off, G):
+    """A recurrent layer: recurrence over packed sequences, then group norm with SiLU per token; and its backward pass."""
+    C = x.shape[1]
+    r, i = gates[:, :C], gates[:, C:]
+    h, hT, saved = s2d.seq_recur_fwd(x, r, i, lam, offsets=off, want_final=True, want_saved=True)
+    y, stats = s2d.group_norm_fwd(h[:, None], gamma, beta, G, act=s2d.ACT_SILU)
+    dh, dgamma, dbeta = s2d.group_norm_bwd(h[:, None], gamma, beta, G, stats, dy[:, None], act=s2d.ACT_SILU)
+    dgates = torch.empty_like(gates)
+    dx, _, _, dlam, _ = s2d.seq_recur_bwd(x, r, i, lam, dh[:, 0], saved, offsets=off, out=(None, dgates[:, :C], dgates[:, C:]))
+    return dict(h=h, hT=hT, y=y[:, 0], dh=dh[:, 0], dx=dx, dgates=dgates, dlam=dlam, dgamma=dgamma, dbeta=dbeta)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_recurrence_and_norm_in_a_row_match_the_oracle(torch, s2d, dtype):
+    rng = np.random.default_rng(23)
+    lens, C, G = [130, 1, 0, 261, 40], 160, 5
+    T = sum(lens)
+    v = chain_inputs(torch, rng, T, C, dtype)
+    x, gates, dy, lam, gamma, beta = v
+    off = torch.tensor([0, *np.cumsum(lens)], dtype=torch.int32, device="cuda")
+    got = chain(torch, s2d, *v, off, G)
+    torch.cuda.synchronize()
+    # each stage against the oracle on the tensors that this run handed it
+    norm = seq.group_norm(host(got["h"])[:, None], host(gamma), host(beta), G, 1e-5, "silu", dy=host(dy)[:, None])
+    rec = seq.recur(host(x), host(gates)[:, :C], host(gates)[:, C:], host(lam), spans_of("packed", lens), dh=host(got["dh"]))
+    close("h", got["h"], rec["h"], dtype)
+    close("y", got["y"], tuple(t[:, 0] for t in norm["y"]), dtype)
+    close("dh", got["dh"], tuple(t[:, 0] for t in norm["dx"]), dtype)
+    close("dx", got["dx"], rec["dx"], dtype)
+    close("dr", got["dgates"][:, :C], rec["dr"], dtype)
+    close("di", got["dgates"][:, C:], rec["di"], dtype)
+    for name, ref in (("hT", rec["hT"]), ("dlam", rec["dlam"]), ("dgamma", norm["dgamma"]), ("dbeta", norm["dbeta"])):
+        close(name, got[name], ref, "fp32")
+
+
+@pytest.mark.parametrize("T,C,G", [(40, 64, 4), (5000, 256, 8)])
+def test_captured_and_replayed(torch, s2d, T, C, G):
+    """The layer's forward and backward, a grid's group norm and a decode step in one graph, replayed on new values between
+    eager work; two graphs that share one memory pool."""
+    rng = np.random.default_rng(29)
+    off = torch.tensor([0, T // 3, T], dtype=torch.int32, device="cuda")
+    still = [chain_inputs(torch, rng, T, C, "bf16") for _ in range(2)]
+    grid = [rows(torch, rng, (2, T, C), "bf16") for _ in range(2)]
+    state = [torch.zeros(8, C, device="cuda") for _ in range(2)]
+
+    def work(k):
+        out = chain(torch, s2d, *still[k], off, G)
+        out["grid"], stats = s2d.group_norm_fwd(grid[k], None, None, G, act=s2d.ACT_GELU)
+        out["dgrid"], _, _ = s2d.group_norm_bwd(grid[k], None, None, G, stats, grid[k], act=s2d.ACT_GELU)
+        x, gates = still[k][0], still[k][1]
+        out["step"] = s2d.seq_recur_step(x[:8], gates[:8, :C], gates[:8, C:], still[k][3], state[k])
+        return out
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for k in range(2):
+            work(k)
+    torch.cuda.current_stream().wait_stream(side)
+    pool = torch.cuda.graph_pool_handle()
+    graphs, outs = [], []
+    for k in range(2):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, pool=pool):
+            outs.append(work(k))
+        graphs.append(gr)
+    for turn in range(3):
+        for k in range(2):
+            for t, new in zip(still[k], chain_inputs(torch, rng, T, C, "bf16")):
+                t.copy_(new)
+            state[k].fill_(turn + 0.5)
+            torch.cuda.synchronize()
+            graphs[k].replay()
+            torch.cuda.synchronize()
+            got = {n: t.clone() for n, t in outs[k].items()}
+            state[k].fill_(turn + 0.5)
+            want = work(k)
+            torch.cuda.synchronize()
+            for n in want:
+                assert torch.equal(got[n], want[n]), (turn, k, n)
+
+
+def test_two_streams_at_once(torch, s2d):
+    """The same calls on two streams side by side, long enough to overlap, give what each gives alone."""
+    rng = np.random.default_rng(31)
+    T, C, G = 20000, 512, 8
+    off = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    v = [chain_inputs(torch, rng, T, C, "bf16") for _ in range(2)]
+    alone = [chain(torch, s2d, *v[k], off, G) for k in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = [None, None]
+    for turn in range(3):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                both[k] = chain(torch, s2d, *v[k], off, G)
+    torch.cuda.synchronize()
+    for k in range(2):
+        for n in alone[k]:
+            assert torch.equal(alone[k][n], both[k][n]), n
+
+
+def test_binding_refusals(torch, s2d):
+    x = torch.zeros(6, 8, device="cuda")
+    lam = torch.zeros(8, device="cuda")
+    off = torch.tensor([0, 6], dtype=torch.int32, device="cuda")
+    ok = lambda **k: s2d.seq_recur_fwd(**{**dict(x=x, r=x, i=x, lam=lam), **k})
+    ok()
+    for bad, kind in ((dict(x=x.half()), TypeError), (dict(r=x.bfloat16()), ValueError), (dict(i=x[:5]), ValueError), (dict(lam=lam[:7]), ValueError),
+                      (dict(lam=lam.double()), ValueError), (dict(offsets=off.long()), ValueError), (dict(offsets=off[:1]), ValueError),
+                      (dict(lengths=off[:1]), ValueError), (dict(h0=torch.zeros(2, 8, device="cuda")), ValueError), (dict(r=x.cpu()), ValueError),
+                      (dict(x=x.t().contiguous().t()), ValueError), (dict(r=x[:1].expand(6, 8)), ValueError), (dict(offsets=off.cpu()), ValueError),
+                      (dict(x=x[:, None, None]), ValueError), (dict(lam=None), ValueError), (dict(x=lam), ValueError), (dict(scale="a"), TypeError)):
+        with pytest.raises(kind):
+            ok(**bad)
+    for bad, code in ((dict(scale=0.0), -2), (dict(h=x), -2), (dict(x=x[None], r=x[None], i=x[None], offsets=None, scale=float("nan")), -2)):
+        with pytest.raises(s2d.Scan2dError) as e:
+            ok(**bad)
+        assert e.value.code == code
+    _, _, saved = ok(want_saved=True)
+    with pytest.raises(ValueError):
+        s2d.seq_recur_bwd(x, x, x, lam, x, None)
+    with pytest.raises(ValueError):
+        s2d.seq_recur_bwd(x, x, x, lam, x, saved, out=(None, None))
+    with pytest.raises(s2d.Scan2dError) as e:
+        s2d.seq_recur_bwd(x, x, x, lam, x, saved[:0])
+    assert e.value.code in (-1, -5)
+    with pytest.raises(ValueError):
+        s2d.seq_recur_step(x, x, x, lam, torch.zeros(6, 8, device="cuda").bfloat16())
+    with pytest.raises(s2d.Scan2dError):
+        s2d.seq_recur_step(x, x, x, lam, torch.zeros(5, 8, device="cuda"))
+    m = torch.zeros(2, 3, 8, device="cuda")
+    for bad, kind in ((dict(groups=0), ValueError), (dict(groups=9), ValueError), (dict(gamma=lam[:4]), ValueError),
+                      (dict(mask=torch.zeros(2, 4, dtype=torch.uint8, device="cuda")), ValueError),
+                      (dict(mask=torch.zeros(2, 3, device="cuda")), ValueError), (dict(x=x), ValueError)):
+        with pytest.raises(kind):
+            s2d.group_norm_fwd(**{**dict(x=m, gamma=None, beta=None, groups=2), **bad})
+    for bad, code in ((dict(groups=3), -2), (dict(act=7), -4), (dict(eps=-1.0), -2)):
+        with pytest.raises(s2d.Scan2dError) as e:
+            s2d.group_norm_fwd(**{**dict(x=m, gamma=None, beta=None, groups=2), **bad})
+        assert e.value.code == code
