@@ -1,4 +1,24 @@
-// The gated linear recurrence on channels-last rows (include/scan2d_seq.h).
+// The gated linear recurrence on channels-last rows (include/scan2d_seq.h): per channel
+//     a_t = exp(-scale softplus(lam) sigmoid(r_t)),  u_t = sqrt(1 - a_t^2) sigmoid(i_t) x_t,  h_t = a_t h_{t-1} + u_t.
+//
+// Bound: HBM.  Forward 3 reads and 1 write per element, backward 4 and 3, with six elementary functions per element that
+// take about as long as the bytes do in bf16; so every row is read once, and the scan over T is done in one pass.
+//
+// A sequence of maps h -> A h + S composes to one of the same form: (A1, S1) then (A2, S2) is (A1 A2, A2 S1 + S2).  A
+// workgroup takes a chunk of TW x NW consecutive rows (of whatever sequences) x 64 V channels: a wavefront has TW
+// rows, a lane V neighbouring channels of them, all in registers.  Each lane forms the map of its rows, the wavefronts' maps
+// meet in LDS, and the chunk's map (A, S) goes to the workspace, where the chunks behind it pick it up.  The state in front
+// of a chunk is the one behind the last full group of kGroup chunks, which the group's last chunk has written, carried
+// through the maps of the chunks in between, always in this order: the same bits every time.  With the state in hand the lane runs its
+// rows once more from registers and writes them.  The first row of a sequence enters as A = -0, S = a h0 + u, rows of
+// no sequence as A = -0, S = 0, so sequences of any lengths share chunks; the sign marks a map that does not look at
+// what comes before it (0 times a NaN would), where a product of decays that underflows is +0.  The backward pass is the same scan from the last row to the first
+// for e_t = a_t (dh_t + e_{t+1}); it rebuilds the states from the ones in front of each chunk, which the forward saved.
+//
+// No wait without an end: a workgroup draws its chunk from its columns' counter, so every chunk it waits for belongs to
+// a workgroup that is already running; a chunk's map is written before its workgroup waits for anything, and the state behind
+// a group needs only chunks with smaller numbers.  A word in the workspace holds value and flag together (one 64-bit
+// store), set to "not written" by a kernel in front of the pass.
 #include "scan2d_seq.hpp"
 
 #include "scan2d_block.hpp"
@@ -7,81 +27,482 @@
 namespace scan2d {
 namespace {
 
-__device__ __forceinline__ float load1(const float* p) { return *p; }
-__device__ __forceinline__ float load1(const bf16_t* p) { return __uint_as_float((uint32_t)p->bits << 16); }
+constexpr int kGroup = 16;               // chunks between the states that the chain hands on
+constexpr int kSavedRows = 64;           // rows between the states that the forward saves: a chunk of the backward
 
 __device__ __forceinline__ float sigmoid(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t * kLog2e)); }
 
-// Per channel: scale * softplus(lam), and sigmoid(lam) / softplus(lam) (-> 1 for lam -> -inf).
-__device__ __forceinline__ float decay_of(float lam, float scale) { return scale * (lam > 20.0f ? lam : log1pf(expf(lam))); }
+// Per channel: scale * softplus(lam) in powers of two, and sigmoid(lam) / softplus(lam) (-> 1 for lam -> -inf).
+__device__ __forceinline__ float decay_of(float lam, float scale) { return scale * (lam > 20.0f ? lam : log1pf(expf(lam))) * kLog2e; }
 __device__ __forceinline__ float decay_slope(float lam) { return lam < -15.0f ? 1.0f : 1.0f / ((1.0f + expf(-lam)) * (lam > 20.0f ? lam : log1pf(expf(lam)))); }
 
-// 1 - e^z for z <= 0, without the cancellation near 0: the series of (e^z - 1) / z to degree 6 on [-0.5, 0] (the next term is
-// below 2e-7); beyond, 1 - e^z >= 0.39.
-__device__ __forceinline__ float one_minus_exp(float z, float ez) {
-    const float p = 1.0f + z * (0.5f + z * (0.16666667f + z * (0.041666668f + z * (0.008333334f + z * (0.0013888889f + z * 0.0001984127f)))));
-    return z > -0.5f ? -z * p : 1.0f - ez;
+// 1 - 2^(2y) for y <= 0 without the cancellation near 0, a = 2^y: -y p(y), p the Chebyshev fit of degree 5 to
+// (1 - 2^(2y)) / -y on [-0.5, 0] (off by 1.1e-8); beyond, 1 - a^2 >= 0.5 loses nothing.
+__device__ __forceinline__ float one_minus_square(float y, float a) {
+    float p = fmaf(y, 0.007358775474131107f, 0.0413372628390789f);
+    p = fmaf(y, p, 0.15355470776557922f);
+    p = fmaf(y, p, 0.4439942240715027f);
+    p = fmaf(y, p, 0.9609044194221497f);
+    p = fmaf(y, p, 1.3862943649291992f);
+    return y > -0.5f ? -y * p : fmaf(-a, a, 1.0f);
 }
 
-struct Rows { int lo, hi; };
-__device__ __forceinline__ Rows rows_of(const RecurArgs& p, int s) {
+// V neighbouring elements as loaded.
+template <typename T, int V> struct Pack { uint32_t w[V * Elem<T>::kBytes <= 4 ? 1 : V * Elem<T>::kBytes / 4]; };
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const void* row, uint32_t offset) {
+    const char* p = static_cast<const char*>(row) + offset;
+    Pack<T, V> r;
+    if constexpr (V * Elem<T>::kBytes == 2) r.w[0] = *reinterpret_cast<const uint16_t*>(p);
+    else load_words_any<V * Elem<T>::kBytes / 4>(p, r.w);
+    return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ float get(const Pack<T, V>& r, int j) { return get_elem<T, V>(r.w, j); }
+template <typename T, int V>
+__device__ __forceinline__ void store_pack(void* row, uint32_t offset, const float* v) {
+    char* p = static_cast<char*>(row) + offset;
+    if constexpr (Elem<T>::kBytes == 4) store_words_any<V>(p, reinterpret_cast<const uint32_t*>(v));
+    else if constexpr (V == 1) *reinterpret_cast<uint16_t*>(p) = (uint16_t)f32_to_bf16_bits(v[0]);
+    else {
+        uint32_t w[V / 2];
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+        store_words_any<V / 2>(p, w);
+    }
+}
+
+// ---- maps h -> A h + S
+constexpr float kCut = -0.0f;            // A of a map that forgets h
+__device__ __forceinline__ bool is_cut(float A) { return (int32_t)__float_as_uint(A) < 0; }
+__device__ __forceinline__ float apply(float A, float h, float S) { return is_cut(A) ? S : fmaf(A, h, S); }
+__device__ __forceinline__ float compose(float first, float then) { return is_cut(then) ? then : first * then; }
+
+// ---- the rows' sequences
+struct Span { int lo, hi; };
+__device__ __forceinline__ Span span_of(const RecurArgs& p, int s) {
     if (p.offsets) return {min(max(p.offsets[s], 0), p.T), min(max(p.offsets[s + 1], 0), p.T)};
     const int lo = s * p.per;
     return {lo, lo + (p.lengths ? min(max(p.lengths[s], 0), p.per) : p.per)};
 }
-
-template <typename T>
-__global__ __launch_bounds__(64) void recur_fwd_kernel(const RecurArgs p) {
-    const int c = (blockIdx.x % ((p.C + 63) / 64)) * 64 + threadIdx.x, s = blockIdx.x / ((p.C + 63) / 64);
-    if (c >= p.C) return;
-    const Rows w = rows_of(p, s);
-    const float decay = decay_of(p.lam[c], p.scale);
-    float h = p.h0 ? p.h0[(size_t)s * p.C + c] : 0.0f;
-    for (int t = w.lo; t < w.hi; ++t) {
-        const float x = load1(static_cast<const T*>(p.x) + t * p.sx + c), sr = sigmoid(load1(static_cast<const T*>(p.r) + t * p.sr + c)),
-                    si = sigmoid(load1(static_cast<const T*>(p.i) + t * p.si + c));
-        const float la = -decay * sr, a = __builtin_amdgcn_exp2f(la * kLog2e);
-        if (p.saved) p.saved[(size_t)t * p.C + c] = h;
-        h = fmaf(a, h, sqrtf(one_minus_exp(2.0f * la, a * a)) * si * x);
-        store_elem(static_cast<T*>(p.h) + t * p.sh + c, h);
+// What the TW rows of a wavefront from t0 on are, a bit for each, and each row's sequence in lane (row - t0).
+struct RowBits {
+    uint64_t first, last, inside;
+    int seq;
+    __device__ __forceinline__ int seq_of(int j) const { return __builtin_amdgcn_readlane(seq, j); }
+};
+template <int TW>
+__device__ __forceinline__ RowBits row_bits(const RecurArgs& p, int t0) {
+    const int lane = threadIdx.x & 63, t = t0 + lane;
+    bool first = false, last = false, inside = false;
+    int s = 0;
+    if (lane < TW && t < p.T) {
+        if (p.offsets) {
+            int lo = 0, hi = p.S;                          // the number of ends offsets[1..S] at or before t
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (p.offsets[mid + 1] <= t) lo = mid + 1; else hi = mid;
+            }
+            s = lo;
+        } else {
+            s = t / p.per;
+        }
+        if (s < p.S) {
+            const Span w = span_of(p, s);
+            inside = t >= w.lo && t < w.hi;
+            first = inside && t == w.lo;
+            last = inside && t + 1 == w.hi;
+        }
     }
-    if (p.hT) p.hT[(size_t)s * p.C + c] = h;
+    return {__ballot(first), __ballot(last), __ballot(inside), s};
 }
 
-template <typename T>
-__global__ __launch_bounds__(64) void recur_bwd_kernel(const RecurArgs p) {
-    const int c = (blockIdx.x % ((p.C + 63) / 64)) * 64 + threadIdx.x, s = blockIdx.x / ((p.C + 63) / 64);
-    if (c >= p.C) return;
-    const Rows w = rows_of(p, s);
-    const float decay = decay_of(p.lam[c], p.scale);
-    float e = p.dhT ? p.dhT[(size_t)s * p.C + c] : 0.0f, sum = 0.0f;      // e: gradient that reaches the state behind token t
-    for (int t = w.hi - 1; t >= w.lo; --t) {
-        const float x = load1(static_cast<const T*>(p.x) + t * p.sx + c), sr = sigmoid(load1(static_cast<const T*>(p.r) + t * p.sr + c)),
-                    si = sigmoid(load1(static_cast<const T*>(p.i) + t * p.si + c));
-        const float la = -decay * sr, a = __builtin_amdgcn_exp2f(la * kLog2e), b2 = one_minus_exp(2.0f * la, a * a);
-        const float ib = b2 > 1.2e-38f ? 1.0f / sqrtf(b2) : 0.0f, b = b2 * ib;
-        const float g = load1(static_cast<const T*>(p.dh) + t * p.sdh + c) + e, before = p.saved[(size_t)t * p.C + c];
-        e = a * g;
-        const float q = la * (e * before - a * a * ib * g * si * x);
-        sum += q;
-        store_elem(static_cast<T*>(p.dx) + t * p.sdx + c, b * si * g);
-        store_elem(static_cast<T*>(p.di) + t * p.sdi + c, b * x * g * si * (1.0f - si));
-        store_elem(static_cast<T*>(p.dr) + t * p.sdr + c, q * (1.0f - sr));
+// The states of sequences of no rows go through: to[s] = from[s].  Wavefront `part` of `parts` looks at every parts-th 64 of them.
+template <int V>
+__device__ __forceinline__ void pass_empty(const RecurArgs& p, const float* from, float* to, int c, long long part, long long parts) {
+    for (long long base = part * 64; base < p.S; base += parts * 64) {
+        const long long s = base + (threadIdx.x & 63);
+        bool empty = false;
+        if (s < p.S) {
+            const Span w = span_of(p, (int)s);
+            empty = w.lo >= w.hi;
+        }
+        for (uint64_t m = __ballot(empty); m != 0; m &= m - 1) {
+            const size_t at = (size_t)(base + __builtin_ctzll(m)) * p.C + c;
+#pragma unroll
+            for (int v = 0; v < V; ++v) to[at + v] = from ? from[at + v] : 0.0f;
+        }
     }
-    if (p.dh0) p.dh0[(size_t)s * p.C + c] = e;
-    static_cast<float*>(p.workspace)[(size_t)s * p.C + c] = sum;
 }
 
-__global__ __launch_bounds__(64) void recur_dlam_kernel(const float* parts, int n, int C, const float* lam, float* dlam) {
-    const int c = blockIdx.x * 64 + threadIdx.x;
-    if (c >= C) return;
+// ---- the chain of chunks
+// Workspace: a counter per column of workgroups (64 bytes each), then per chunk and channel the map (A, S), then per
+// group and channel the state behind it.  All bits set: not written.
+constexpr uint32_t kUnset = 0xffffffffu;
+__host__ __device__ inline size_t chain_counters(int cols) { return (size_t)cols * 8; }               // in 64-bit words
+__host__ __device__ inline size_t chain_words(int chunks, int cols, int width) {
+    return chain_counters(cols) + ((size_t)chunks + (size_t)(chunks + kGroup - 1) / kGroup) * cols * width;
+}
+
+__device__ __forceinline__ uint64_t chain_word(float hi, float lo) {
+    uint32_t h = __float_as_uint(hi);
+    if (hi != hi) h = 0x7fc00000u;                          // a NaN, but not the one that means "not written"
+    return ((uint64_t)h << 32) | __float_as_uint(lo);
+}
+__device__ __forceinline__ void chain_put(uint64_t* w, uint64_t v) { __hip_atomic_store(w, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <int V>
+__device__ __forceinline__ void chain_get(const uint64_t* w, uint64_t* v) {
+    for (;;) {
+        bool all = true;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            v[k] = __hip_atomic_load(w + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            all = all && (uint32_t)(v[k] >> 32) != kUnset;
+        }
+        if (__all(all)) return;
+        __builtin_amdgcn_s_sleep(1);
+    }
+}
+
+__global__ __launch_bounds__(256) void recur_clear_kernel(uint4* w, size_t n) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) w[i] = make_uint4(kUnset, kUnset, kUnset, kUnset);
+}
+
+template <int V, int NW>
+struct ChainLds {
+    float A[kGroup][64 * V], S[kGroup][64 * V];
+    int ticket;
+};
+// The chunk this workgroup is to do: the next of its column's.
+template <int V, int NW>
+__device__ __forceinline__ int chain_ticket(uint64_t* ws, int col, ChainLds<V, NW>& lds) {
+    if (threadIdx.x == 0) lds.ticket = (int)(atomicAdd(reinterpret_cast<uint32_t*>(ws + (size_t)col * 8), 1u) + 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(lds.ticket);
+}
+// The value in front of chunk k (in the order of the scan) for this lane's channels, where the map of chunk k itself is
+// (A, S); every wavefront gets it.  `needed` (the same for the whole workgroup): whether chunk k has use for it.
+template <int V, int NW>
+__device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int col, int k, bool needed, const float* A, const float* S, float* carry,
+                                      ChainLds<V, NW>& lds) {
+    constexpr int WIDTH = 64 * V;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = k / kGroup, j = k % kGroup;
+    uint64_t* maps = ws + chain_counters(cols) + (size_t)col * WIDTH + lane * V;
+    uint64_t* states = maps + (size_t)chunks * cols * WIDTH;
+    const size_t step = (size_t)cols * WIDTH;
+    const bool end = j == kGroup - 1 || k == chunks - 1;    // nobody reads the map of a group's last chunk
+    if (wave == 0 && !end) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) chain_put(maps + (size_t)k * step + v, chain_word(A[v], S[v]));
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry[v] = 0.0f;
+    const bool hand_on = j == kGroup - 1 && k != chunks - 1;
+    if (needed) {
+        // slot 0: the state behind the group before; slot m: the map of the group's chunk m - 1
+        for (int m = wave; m <= j; m += NW) {
+            if (m == 0 && g == 0) continue;
+            uint64_t w[V];
+            chain_get<V>(m == 0 ? states + (size_t)(g - 1) * step : maps + (size_t)(g * kGroup + m - 1) * step, w);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                lds.A[m][lane * V + v] = __uint_as_float((uint32_t)(w[v] >> 32));
+                lds.S[m][lane * V + v] = __uint_as_float((uint32_t)w[v]);
+            }
+        }
+        __syncthreads();
+        if (g > 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) carry[v] = lds.S[0][lane * V + v];
+        }
+        for (int m = 1; m <= j; ++m)
+#pragma unroll
+            for (int v = 0; v < V; ++v) carry[v] = apply(lds.A[m][lane * V + v], carry[v], lds.S[m][lane * V + v]);
+    }
+    if (wave == 0 && hand_on) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) chain_put(states + (size_t)g * step + v, chain_word(0.0f, apply(A[v], carry[v], S[v])));
+    }
+}
+
+// ---- forward
+template <typename T, int V, int TW, int NW>
+__global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, int chunks, int cols) {
+    constexpr int WIDTH = 64 * V;
+    __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH];
+    __shared__ ChainLds<V, NW> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
+    uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
+    const int k = chunks > 1 ? chain_ticket<V, NW>(ws, col, lds) : 0;
+    const int c = min(col * WIDTH + lane * V, p.C - V);     // the lanes past the last channels do those again
+    const uint32_t off = (uint32_t)c * Elem<T>::kBytes;
+    const int t0 = (k * NW + wave) * TW;
+    Pack<T, V> xr[TW], rr[TW], ir[TW];
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+        const long long t = min(t0 + j, p.T - 1);
+        xr[j] = load_pack<T, V>(static_cast<const T*>(p.x) + t * p.sx, off);
+        rr[j] = load_pack<T, V>(static_cast<const T*>(p.r) + t * p.sr, off);
+        ir[j] = load_pack<T, V>(static_cast<const T*>(p.i) + t * p.si, off);
+    }
+    const RowBits bits = row_bits<TW>(p, t0);
+    float decay[V], A[V], S[V], a[TW][V], u[TW][V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) { decay[v] = decay_of(p.lam[c + v], p.scale); A[v] = 1.0f; S[v] = 0.0f; }
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float y = -decay[v] * sigmoid(get<T, V>(rr[j], v)), e = __builtin_amdgcn_exp2f(y);
+            a[j][v] = e;
+            u[j][v] = __builtin_amdgcn_sqrtf(one_minus_square(y, e)) * sigmoid(get<T, V>(ir[j], v)) * get<T, V>(xr[j], v);
+        }
+        if ((bits.first >> j) & 1) {
+            const float* h0 = p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (h0) u[j][v] = fmaf(a[j][v], h0[v], u[j][v]);
+                S[v] = u[j][v];
+                A[v] = kCut;
+            }
+        } else if (!((bits.inside >> j) & 1)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) { u[j][v] = S[v] = 0.0f; A[v] = kCut; }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                S[v] = fmaf(a[j][v], S[v], u[j][v]);
+                A[v] *= a[j][v];
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; }
+    __syncthreads();
+    float h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = 0.0f;
+    if (chunks > 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) { A[v] = 1.0f; S[v] = 0.0f; }
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                S[v] = apply(mapA[w][lane * V + v], S[v], mapS[w][lane * V + v]);
+                A[v] = compose(A[v], mapA[w][lane * V + v]);
+            }
+        chain<V, NW>(ws, chunks, cols, col, k, k > 0, A, S, h, lds);
+    }
+    for (int w = 0; w < wave; ++w)
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = apply(mapA[w][lane * V + v], h[v], mapS[w][lane * V + v]);
+    if (p.saved && t0 % kSavedRows == 0 && t0 < p.T) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) p.saved[(size_t)(t0 / kSavedRows) * p.C + c + v] = h[v];
+    }
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+        const bool cut = (((bits.first | ~bits.inside) >> j) & 1) != 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = cut ? u[j][v] : fmaf(a[j][v], h[v], u[j][v]);
+        if ((bits.inside >> j) & 1) store_pack<T, V>(static_cast<T*>(p.h) + (long long)(t0 + j) * p.sh, off, h);
+        if (p.hT && ((bits.last >> j) & 1)) {
+            float* hT = p.hT + (size_t)bits.seq_of(j) * p.C + c;
+#pragma unroll
+            for (int v = 0; v < V; ++v) hT[v] = h[v];
+        }
+    }
+    if (p.hT) pass_empty<V>(p, p.h0, p.hT, c, (long long)k * NW + wave, (long long)chunks * NW);
+}
+
+// ---- backward
+template <typename T, int V, int TW, int NW>
+__global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, float* parts, int chunks, int cols) {
+    constexpr int WIDTH = 64 * V;
+    __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH], mapD[NW][WIDTH];
+    __shared__ ChainLds<V, NW> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
+    uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
+    const int n = chunks > 1 ? chain_ticket<V, NW>(ws, col, lds) : 0, k = chunks - 1 - n;   // the chain runs from the last chunk
+    const int c = min(col * WIDTH + lane * V, p.C - V);
+    const uint32_t off = (uint32_t)c * Elem<T>::kBytes;
+    const int t0 = (k * NW + wave) * TW;
+    Pack<T, V> xr[TW], rr[TW], ir[TW], dr[TW];
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+        const long long t = min(t0 + j, p.T - 1);
+        xr[j] = load_pack<T, V>(static_cast<const T*>(p.x) + t * p.sx, off);
+        rr[j] = load_pack<T, V>(static_cast<const T*>(p.r) + t * p.sr, off);
+        ir[j] = load_pack<T, V>(static_cast<const T*>(p.i) + t * p.si, off);
+        dr[j] = load_pack<T, V>(static_cast<const T*>(p.dh) + t * p.sdh, off);
+    }
+    const RowBits bits = row_bits<TW>(p, t0);
+    float decay[V], A[V], S[V], D[V], h[V], a[TW][V], u[TW][V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        decay[v] = decay_of(p.lam[c + v], p.scale);
+        h[v] = p.saved[(size_t)k * p.C + c + v];
+        A[v] = 1.0f; S[v] = 0.0f; D[v] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float y = -decay[v] * sigmoid(get<T, V>(rr[j], v)), e = __builtin_amdgcn_exp2f(y);
+            a[j][v] = e;
+            u[j][v] = __builtin_amdgcn_sqrtf(one_minus_square(y, e)) * sigmoid(get<T, V>(ir[j], v)) * get<T, V>(xr[j], v);
+        }
+        if ((bits.first >> j) & 1) {
+            const float* h0 = p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (h0) u[j][v] = fmaf(a[j][v], h0[v], u[j][v]);
+                S[v] = u[j][v];
+                A[v] = kCut;
+            }
+        } else if (!((bits.inside >> j) & 1)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) { u[j][v] = S[v] = 0.0f; A[v] = kCut; }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                S[v] = fmaf(a[j][v], S[v], u[j][v]);
+                A[v] *= a[j][v];
+            }
+        }
+    }
+    // e in front of the rows from the one behind them: D + A e
+    auto grad = [&](int j, int v) { return get<T, V>(dr[j], v); };
+#pragma unroll
+    for (int j = TW - 1; j >= 0; --j) {
+        if (!((bits.inside >> j) & 1) || ((bits.first >> j) & 1)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) D[v] = 0.0f;
+        } else {
+            const float* dT = p.dhT && ((bits.last >> j) & 1) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                // behind a sequence's last row there is another's first, whose e does not come here: D is 0 there
+                D[v] = a[j][v] * (grad(j, v) + D[v] + (dT ? dT[v] : 0.0f));
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; mapD[wave][lane * V + v] = D[v]; }
+    __syncthreads();
+    float e[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) e[v] = 0.0f;
+    if (chunks > 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) { A[v] = 1.0f; D[v] = 0.0f; }
+        for (int w = NW - 1; w >= 0; --w)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                D[v] = apply(mapA[w][lane * V + v], D[v], mapD[w][lane * V + v]);
+                A[v] = compose(A[v], mapA[w][lane * V + v]);
+            }
+        chain<V, NW>(ws, chunks, cols, col, n, n > 0, A, D, e, lds);
+    }
+    for (int w = NW - 1; w > wave; --w)
+#pragma unroll
+        for (int v = 0; v < V; ++v) e[v] = apply(mapA[w][lane * V + v], e[v], mapD[w][lane * V + v]);
+    for (int w = 0; w < wave; ++w)
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = apply(mapA[w][lane * V + v], h[v], mapS[w][lane * V + v]);
+    // the state in front of each row takes the place of its u
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+        const bool cut = ((bits.first >> j) & 1) || !((bits.inside >> j) & 1);
+        const float* h0 = cut && p.h0 && ((bits.first >> j) & 1) ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float next = cut ? u[j][v] : fmaf(a[j][v], h[v], u[j][v]);
+            u[j][v] = cut ? (h0 ? h0[v] : 0.0f) : h[v];
+            h[v] = next;
+        }
+    }
+    float sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+#pragma unroll
+    for (int j = TW - 1; j >= 0; --j) {
+        if (!((bits.inside >> j) & 1)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) e[v] = 0.0f;
+            continue;
+        }
+        const float* dT = p.dhT && ((bits.last >> j) & 1) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+        float dx[V], di[V], dg[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float sr = sigmoid(get<T, V>(rr[j], v)), si = sigmoid(get<T, V>(ir[j], v)), x = get<T, V>(xr[j], v);
+            const float y = -decay[v] * sr, av = a[j][v], b2 = one_minus_square(y, av);
+            const float ib = b2 > 1.2e-38f ? __builtin_amdgcn_rsqf(b2) : 0.0f, b = b2 * ib;
+            const float g = grad(j, v) + e[v] + (dT ? dT[v] : 0.0f);
+            e[v] = av * g;
+            const float gs = g * si, q = y * 0.6931471805599453f * (e[v] * u[j][v] - av * av * ib * gs * x);
+            sum[v] += q;
+            dx[v] = b * gs;
+            di[v] = dx[v] * x * (1.0f - si);
+            dg[v] = q * (1.0f - sr);
+        }
+        const long long t = t0 + j;
+        store_pack<T, V>(static_cast<T*>(p.dx) + t * p.sdx, off, dx);
+        store_pack<T, V>(static_cast<T*>(p.di) + t * p.sdi, off, di);
+        store_pack<T, V>(static_cast<T*>(p.dr) + t * p.sdr, off, dg);
+        if ((bits.first >> j) & 1) {
+            if (p.dh0) {
+                float* d0 = p.dh0 + (size_t)bits.seq_of(j) * p.C + c;
+#pragma unroll
+                for (int v = 0; v < V; ++v) d0[v] = e[v];
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) e[v] = 0.0f;
+        }
+    }
+    if (p.dh0) pass_empty<V>(p, p.dhT, p.dh0, c, (long long)k * NW + wave, (long long)chunks * NW);
+    __syncthreads();                                        // the maps have been read
+#pragma unroll
+    for (int v = 0; v < V; ++v) mapA[wave][lane * V + v] = sum[v];
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) total += mapA[w][lane * V + v];
+            if (chunks > 1) parts[(size_t)k * p.C + c + v] = total;
+            else p.dlam[c + v] = total * decay_slope(p.lam[c + v]);
+        }
+    }
+}
+
+// dlam from the chunks' sums: 64 channels x 16 parts of the chunks per workgroup, the parts joined in order.
+__global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* parts, int n, int C, const float* lam, float* dlam) {
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     float sum = 0.0f;
-    for (int k = 0; k < n; ++k) sum += parts[(size_t)k * C + c];
-    dlam[c] = sum * decay_slope(lam[c]);
+    if (c < C)
+        for (int k = w; k < n; k += 16) sum += parts[(size_t)k * C + c];
+    red[w][lane] = sum;
+    __syncthreads();
+    if (w == 0 && c < C) {
+        for (int q = 1; q < 16; ++q) sum += red[q][lane];
+        dlam[c] = sum * decay_slope(lam[c]);
+    }
 }
 
-// One row and 256 channels per workgroup.  A slot that stands at several rows is done by the workgroup of the first of
-// them, in the order of the rows.
+// No rows at all: the states go through, and nothing adds to dlam.
+__global__ __launch_bounds__(256) void recur_none_kernel(const float* from, float* to, long long n, float* zero, int C) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (to && i < n) to[i] = from ? from[i] : 0.0f;
+    if (zero && i < C) zero[i] = 0.0f;
+}
+
+// ---- one token per sequence.  One row and 256 channels per workgroup.  A slot that stands at several rows is done by the
+// workgroup of the first of them, in the order of the rows.
 template <typename T>
 __global__ __launch_bounds__(256) void recur_step_kernel(const RecurArgs p, float* state, const int32_t* slots, long long slot_count) {
     const int cols = (p.C + 255) / 256, row = blockIdx.x / cols, c = (blockIdx.x % cols) * 256 + threadIdx.x;
@@ -94,41 +515,95 @@ __global__ __launch_bounds__(256) void recur_step_kernel(const RecurArgs p, floa
     }
     if (c >= p.C) return;
     const float decay = decay_of(p.lam[c], p.scale);
+    const uint32_t off = (uint32_t)c * Elem<T>::kBytes;
     float h = state[(size_t)slot * p.C + c];
     for (int t = row; t < (slots ? p.T : row + 1); ++t) {
         if (slots && slots[t] != slot) continue;
-        const float x = load1(static_cast<const T*>(p.x) + t * p.sx + c), sr = sigmoid(load1(static_cast<const T*>(p.r) + t * p.sr + c)),
-                    si = sigmoid(load1(static_cast<const T*>(p.i) + t * p.si + c));
-        const float la = -decay * sr, a = __builtin_amdgcn_exp2f(la * kLog2e);
-        h = fmaf(a, h, sqrtf(one_minus_exp(2.0f * la, a * a)) * si * x);
-        store_elem(static_cast<T*>(p.h) + t * p.sh + c, h);
+        const float x = get<T, 1>(load_pack<T, 1>(static_cast<const T*>(p.x) + t * p.sx, off), 0);
+        const float r = get<T, 1>(load_pack<T, 1>(static_cast<const T*>(p.r) + t * p.sr, off), 0);
+        const float i = get<T, 1>(load_pack<T, 1>(static_cast<const T*>(p.i) + t * p.si, off), 0);
+        const float y = -decay * sigmoid(r), a = __builtin_amdgcn_exp2f(y);
+        h = fmaf(a, h, __builtin_amdgcn_sqrtf(one_minus_square(y, a)) * sigmoid(i) * x);
+        store_pack<T, 1>(static_cast<T*>(p.h) + t * p.sh, off, &h);
     }
     state[(size_t)slot * p.C + c] = h;
 }
 
 int launched() { return hipGetLastError() == hipSuccess ? SCAN2D_OK : SCAN2D_ERR_LAUNCH_FAILED; }
 
+// ---- shapes.  One lane per channel up to 64 channels, two channels per lane beyond.
+constexpr int kWaves = 8;                // wavefronts of a workgroup
+constexpr int kFwdRowsF32 = 8, kFwdRowsBf16 = 16, kBwdRows = kSavedRows / kWaves;      // rows of a wavefront
+struct RecurPlan {
+    int V, chunks, cols;
+    int rows;                            // of a chunk
+};
+RecurPlan plan_of(const scan2d_recur_desc* d, int pass) {
+    RecurPlan q;
+    q.V = d->C <= 64 ? 1 : 2;
+    q.rows = (pass == SCAN2D_PASS_BWD ? kBwdRows : d->dtype == SCAN2D_BF16 ? kFwdRowsBf16 : kFwdRowsF32) * kWaves;
+    q.chunks = (int)((d->T + q.rows - 1) / q.rows);
+    q.cols = (d->C + 64 * q.V - 1) / (64 * q.V);
+    return q;
+}
+size_t chain_bytes(const RecurPlan& q) { return q.chunks > 1 ? (chain_words(q.chunks, q.cols, 64 * q.V) * 8 + 255) / 256 * 256 : 0; }
+
+int clear_chain(const RecurPlan& q, void* workspace, hipStream_t stream) {
+    const size_t n = chain_bytes(q) / 16;
+    hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, static_cast<uint4*>(workspace), n);
+    return launched();
+}
+bool plan_fits(const RecurPlan& q) {
+    return launch_fits((long long)q.chunks * q.cols, 64 * kWaves) && launch_fits((long long)(chain_bytes(q) / 4096 + 1), 256);
+}
+
+int launch_none(const RecurArgs& a, const float* from, float* to, float* zero, hipStream_t stream) {
+    const long long n = (long long)a.S * a.C, blocks = ((n > a.C ? n : a.C) + 255) / 256;
+    if (!launch_fits(blocks, 256)) return SCAN2D_ERR_BAD_SHAPE;
+    hipLaunchKernelGGL(recur_none_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, from, to, n, zero, a.C);
+    return launched();
+}
+
 }  // namespace
 
-size_t recur_saved_bytes(const scan2d_recur_desc* d) { return (size_t)d->T * d->C * 4; }
-size_t recur_workspace_bytes(const scan2d_recur_desc* d, int pass) { return pass == SCAN2D_PASS_BWD ? (size_t)d->S * d->C * 4 : 0; }
+size_t recur_saved_bytes(const scan2d_recur_desc* d) { return (size_t)((d->T + kSavedRows - 1) / kSavedRows) * d->C * 4; }
+size_t recur_workspace_bytes(const scan2d_recur_desc* d, int pass) {
+    const RecurPlan q = plan_of(d, pass);
+    return chain_bytes(q) + (pass == SCAN2D_PASS_BWD && q.chunks > 1 ? (size_t)q.chunks * d->C * 4 : 0);
+}
 
 int recur_fwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t stream) {
-    const long long blocks = (long long)((a.C + 63) / 64) * a.S;
-    if (!launch_fits(blocks, 64)) return SCAN2D_ERR_BAD_SHAPE;
+    const RecurPlan q = plan_of(d, SCAN2D_PASS_FWD);
     (void)hipGetLastError();
-    if (d->dtype == SCAN2D_BF16) hipLaunchKernelGGL(recur_fwd_kernel<bf16_t>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL(recur_fwd_kernel<float>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
+    if (q.chunks == 0) return a.hT ? launch_none(a, a.h0, a.hT, nullptr, stream) : SCAN2D_OK;
+    if (!plan_fits(q)) return SCAN2D_ERR_BAD_SHAPE;
+    if (q.chunks > 1) {
+        const int rc = clear_chain(q, a.workspace, stream);
+        if (rc != SCAN2D_OK) return rc;
+    }
+    using Kernel = void (*)(const RecurArgs, int, int);
+    const Kernel k = d->dtype == SCAN2D_BF16 ? (q.V == 1 ? recur_fwd_kernel<bf16_t, 1, kFwdRowsBf16, kWaves> : recur_fwd_kernel<bf16_t, 2, kFwdRowsBf16, kWaves>)
+                                             : (q.V == 1 ? recur_fwd_kernel<float, 1, kFwdRowsF32, kWaves> : recur_fwd_kernel<float, 2, kFwdRowsF32, kWaves>);
+    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * kWaves), 0, stream, a, q.chunks, q.cols);
     return launched();
 }
 
 int recur_bwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t stream) {
-    const long long blocks = (long long)((a.C + 63) / 64) * a.S;
-    if (!launch_fits(blocks, 64)) return SCAN2D_ERR_BAD_SHAPE;
+    const RecurPlan q = plan_of(d, SCAN2D_PASS_BWD);
     (void)hipGetLastError();
-    if (d->dtype == SCAN2D_BF16) hipLaunchKernelGGL(recur_bwd_kernel<bf16_t>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL(recur_bwd_kernel<float>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
-    hipLaunchKernelGGL(recur_dlam_kernel, dim3((a.C + 63) / 64), dim3(64), 0, stream, static_cast<const float*>(a.workspace), a.S, a.C, a.lam, a.dlam);
+    if (q.chunks == 0) return launch_none(a, a.dhT, a.dh0, a.dlam, stream);
+    if (!plan_fits(q)) return SCAN2D_ERR_BAD_SHAPE;
+    float* parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + chain_bytes(q));
+    if (q.chunks > 1) {
+        const int rc = clear_chain(q, a.workspace, stream);
+        if (rc != SCAN2D_OK) return rc;
+    }
+    using Kernel = void (*)(const RecurArgs, float*, int, int);
+    const Kernel k = d->dtype == SCAN2D_BF16 ? (q.V == 1 ? recur_bwd_kernel<bf16_t, 1, kBwdRows, kWaves> : recur_bwd_kernel<bf16_t, 2, kBwdRows, kWaves>)
+                                             : (q.V == 1 ? recur_bwd_kernel<float, 1, kBwdRows, kWaves> : recur_bwd_kernel<float, 2, kBwdRows, kWaves>);
+    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * kWaves), 0, stream, a, parts, q.chunks, q.cols);
+    if (q.chunks > 1)
+        hipLaunchKernelGGL(recur_dlam_kernel, dim3((a.C + 63) / 64), dim3(1024), 0, stream, parts, q.chunks, a.C, a.lam, a.dlam);
     return launched();
 }
 
