@@ -9,7 +9,7 @@
  * current device has to be the one that owns the pointers.
  *
  * Rows: element (t, c) of a tensor lies at base + t * stride + c, in elements.  Every tensor has a stride of its own, at
- * least C (0 stands for C), so that the halves of a projection [T][2 C] are used where they lie.  These tensors need
+ * least C and below 2^26 (0 stands for C), so that the halves of a projection [T][2 C] are used where they lie.  These tensors need
  * the alignment of their element type only; all others (parameters, states, statistics: dense) that of their type,
  * `saved` and `workspace` 16 bytes.
  */

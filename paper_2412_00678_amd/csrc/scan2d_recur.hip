@@ -47,28 +47,37 @@ __device__ __forceinline__ float one_minus_square(float y, float a) {
     return y > -0.5f ? -y * p : fmaf(-a, a, 1.0f);
 }
 
-// V neighbouring elements as loaded.
+// V neighbouring elements as loaded.  The row's address is the same for the whole wavefront (scalar registers), the lane's
+// offset in it 32 bits.
+typedef __attribute__((address_space(1))) const char* gconst;
+typedef __attribute__((address_space(1))) char* gmut;
+typedef uint16_t u16_a1 __attribute__((aligned(2)));
 template <typename T, int V> struct Pack { uint32_t w[V * Elem<T>::kBytes <= 4 ? 1 : V * Elem<T>::kBytes / 4]; };
 template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> load_pack(const void* row, uint32_t offset) {
-    const char* p = static_cast<const char*>(row) + offset;
+__device__ __forceinline__ Pack<T, V> load_pack(uint64_t row, uint32_t offset) {
+    const gconst p = (gconst)row + offset;
     Pack<T, V> r;
-    if constexpr (V * Elem<T>::kBytes == 2) r.w[0] = *reinterpret_cast<const uint16_t*>(p);
-    else load_words_any<V * Elem<T>::kBytes / 4>(p, r.w);
+    if constexpr (V * Elem<T>::kBytes == 2) r.w[0] = *reinterpret_cast<__attribute__((address_space(1))) const u16_a1*>(p);
+    else if constexpr (V * Elem<T>::kBytes == 4) r.w[0] = *reinterpret_cast<__attribute__((address_space(1))) const u32_a1*>(p);
+    else {
+        static_assert(V * Elem<T>::kBytes == 8, "two dwords");
+        const u32x2_a1 v = *reinterpret_cast<__attribute__((address_space(1))) const u32x2_a1*>(p);
+        r.w[0] = v.x; r.w[1] = v.y;
+    }
     return r;
 }
 template <typename T, int V>
 __device__ __forceinline__ float get(const Pack<T, V>& r, int j) { return get_elem<T, V>(r.w, j); }
 template <typename T, int V>
-__device__ __forceinline__ void store_pack(void* row, uint32_t offset, const float* v) {
-    char* p = static_cast<char*>(row) + offset;
-    if constexpr (Elem<T>::kBytes == 4) store_words_any<V>(p, reinterpret_cast<const uint32_t*>(v));
-    else if constexpr (V == 1) *reinterpret_cast<uint16_t*>(p) = (uint16_t)f32_to_bf16_bits(v[0]);
+__device__ __forceinline__ void store_pack(uint64_t row, uint32_t offset, const float* v) {
+    const gmut p = (gmut)row + offset;
+    if constexpr (V == 1 && Elem<T>::kBytes == 2) *reinterpret_cast<__attribute__((address_space(1))) u16_a1*>(p) = (uint16_t)f32_to_bf16_bits(v[0]);
+    else if constexpr (V == 1) *reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p) = __float_as_uint(v[0]);
+    else if constexpr (Elem<T>::kBytes == 2) *reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p) = pack_bf16x2(v[0], v[1]);
     else {
-        uint32_t w[V / 2];
-#pragma unroll
-        for (int k = 0; k < V / 2; ++k) w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
-        store_words_any<V / 2>(p, w);
+        u32x2_a1 w;
+        w.x = __float_as_uint(v[0]); w.y = __float_as_uint(v[1]);
+        *reinterpret_cast<__attribute__((address_space(1))) u32x2_a1*>(p) = w;
     }
 }
 
@@ -89,33 +98,97 @@ __device__ __forceinline__ Span span_of(const RecurArgs& p, int s) {
 struct RowBits {
     uint64_t first, last, inside;
     int seq;
+    bool plain;                          // rows of one sequence, neither its first nor its last among them
     __device__ __forceinline__ int seq_of(int j) const { return __builtin_amdgcn_readlane(seq, j); }
 };
-template <int TW>
-__device__ __forceinline__ RowBits row_bits(const RecurArgs& p, int t0) {
-    const int lane = threadIdx.x & 63, t = t0 + lane;
-    bool first = false, last = false, inside = false;
-    int s = 0;
-    if (lane < TW && t < p.T) {
+// Finds a row's sequence, which is the number of ends offsets[1..S] at or before it: 64 of them at a time, evenly spaced
+// over what is left.  The first 64 are asked for before the row is known; for up to 64 sequences they are all.
+struct SeqSearch {
+    int step, end, begin;                // lane l has the last of the l-th `step` ends
+    __device__ __forceinline__ explicit SeqSearch(const RecurArgs& p) {
+        const int lane = threadIdx.x & 63;
+        step = (p.S + 63) / 64;
+        end = 0x7fffffff;
+        begin = 0;
         if (p.offsets) {
-            int lo = 0, hi = p.S;                          // the number of ends offsets[1..S] at or before t
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (p.offsets[mid + 1] <= t) lo = mid + 1; else hi = mid;
-            }
-            s = lo;
+            const int at = (lane + 1) * step - 1;
+            if (at < p.S) end = p.offsets[at + 1];
+            begin = p.offsets[0];
+        }
+    }
+    __device__ __forceinline__ int at(const RecurArgs& p, int t) const {
+        // ends ascend, so the lanes that are past come first; where they do not, this is some number of them
+        int lo = __builtin_popcountll(__ballot(end <= t)) * step, n = min(step - 1, max(p.S - lo, 0));
+        while (n > 0) {
+            const int part = (n + 63) / 64, k = lo + ((int)(threadIdx.x & 63) + 1) * part - 1;
+            const int full = __builtin_popcountll(__ballot(k < lo + n && p.offsets[min(k, p.S - 1) + 1] <= t));
+            lo += full * part;
+            n = min(part - 1, max(p.S - lo, 0));
+        }
+        return min(lo, p.S);
+    }
+};
+template <int TW>
+__device__ __forceinline__ RowBits row_bits(const RecurArgs& p, const SeqSearch& search, int t0) {
+    const int lane = threadIdx.x & 63, t = t0 + lane;
+    RowBits r;
+    int s0 = 0, lo, hi;
+    if (p.offsets) {
+        s0 = search.at(p, t0);
+        if (p.S <= 64) {
+            hi = s0 < p.S ? __builtin_amdgcn_readlane(search.end, min(s0, 63)) : -1;
+            lo = s0 > 0 ? __builtin_amdgcn_readlane(search.end, s0 - 1) : search.begin;
         } else {
+            hi = s0 < p.S ? p.offsets[s0 + 1] : -1;
+            lo = p.offsets[s0];
+        }
+        lo = max(lo, 0);
+        hi = min(hi, p.T);
+    } else {
+        s0 = p.per > 0 ? t0 / p.per : 0;
+        lo = s0 * p.per;
+        hi = s0 < p.S ? lo + (p.lengths ? min(max(p.lengths[s0], 0), p.per) : p.per) : -1;
+    }
+    r.plain = lo < t0 && t0 + TW < hi;
+    r.seq = s0;
+    r.first = r.last = 0;
+    r.inside = ~0ull;
+    if (!r.plain) {
+        int s = s0;
+        if (p.offsets) {
+            while (lane < TW && s < p.S && p.offsets[s + 1] <= t) ++s;     // past the ends between t0 and this row
+        } else if (p.per > 0) {
             s = t / p.per;
         }
-        if (s < p.S) {
+        bool first = false, last = false, inside = false;
+        if (lane < TW && t < p.T && s < p.S) {
             const Span w = span_of(p, s);
             inside = t >= w.lo && t < w.hi;
             first = inside && t == w.lo;
             last = inside && t + 1 == w.hi;
         }
+        r.seq = s;
+        r.first = __ballot(first);
+        r.last = __ballot(last);
+        r.inside = __ballot(inside);
     }
-    return {__ballot(first), __ballot(last), __ballot(inside), s};
+    return r;
 }
+// The rows of a tensor from t0 on: one address for the first of them, 32-bit offsets from there (strides are below 2^26 elements, so
+// 15 rows are less than 2^32 bytes).
+struct RowPointer {
+    uint64_t at;
+    uint32_t step;
+    int left;                            // rows behind t0
+    __device__ __forceinline__ RowPointer(const void* base, long long stride, int bytes, int t0, int T) {
+        const int t = min(t0, T - 1);
+        step = (uint32_t)stride * (uint32_t)bytes;
+        at = (uint64_t)base + (uint64_t)t * step;
+        left = T - 1 - t;
+    }
+    __device__ __forceinline__ uint32_t row(int j) const { return (uint32_t)j * step; }
+    __device__ __forceinline__ uint32_t row_or_last(int j) const { return (uint32_t)min(j, left) * step; }     // behind the last row, that one
+};
 
 // The states of sequences of no rows go through: to[s] = from[s].  Wavefront `part` of `parts` looks at every parts-th 64 of them.
 template <int V>
@@ -169,23 +242,27 @@ __global__ __launch_bounds__(256) void recur_clear_kernel(uint4* w, size_t n) {
     if (i < n) w[i] = make_uint4(kUnset, kUnset, kUnset, kUnset);
 }
 
-template <int V, int NW>
+template <int V>
 struct ChainLds {
     float A[kGroup][64 * V], S[kGroup][64 * V];
+    float decay[64 * V];
     int ticket;
 };
-// The chunk this workgroup is to do: the next of its column's.
-template <int V, int NW>
-__device__ __forceinline__ int chain_ticket(uint64_t* ws, int col, ChainLds<V, NW>& lds) {
-    if (threadIdx.x == 0) lds.ticket = (int)(atomicAdd(reinterpret_cast<uint32_t*>(ws + (size_t)col * 8), 1u) + 1u);
+// The chunk this workgroup is to do, the next of its column's, and its channels' decays.
+template <int V>
+__device__ __forceinline__ int chain_start(const RecurArgs& p, uint64_t* ws, int chunks, int cols, int col, ChainLds<V>& lds) {
+    constexpr int WIDTH = 64 * V;
+    if (chunks > 1 && threadIdx.x == 0) lds.ticket = (int)(atomicAdd(reinterpret_cast<uint32_t*>(ws + (size_t)col * 8), 1u) + 1u);
+    const int c = (int)blockDim.x - 1 - (int)threadIdx.x;   // from the last wavefront on: the first waits for its ticket
+    if (c < WIDTH) lds.decay[c] = decay_of(p.lam[min(min(col * WIDTH + c / V * V, p.C - V) + c % V, p.C - 1)], p.scale);
     __syncthreads();
-    return __builtin_amdgcn_readfirstlane(lds.ticket);
+    return chunks > 1 ? __builtin_amdgcn_readfirstlane(lds.ticket) : 0;
 }
 // The value in front of chunk k (in the order of the scan) for this lane's channels, where the map of chunk k itself is
 // (A, S); every wavefront gets it.  `needed` (the same for the whole workgroup): whether chunk k has use for it.
 template <int V, int NW>
 __device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int col, int k, bool needed, const float* A, const float* S, float* carry,
-                                      ChainLds<V, NW>& lds) {
+                                      ChainLds<V>& lds) {
     constexpr int WIDTH = 64 * V;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = k / kGroup, j = k % kGroup;
     uint64_t* maps = ws + chain_counters(cols) + (size_t)col * WIDTH + lane * V;
@@ -226,66 +303,108 @@ __device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int co
     }
 }
 
-// ---- forward
-template <typename T, int V, int TW, int NW>
-__global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, int chunks, int cols) {
-    constexpr int WIDTH = 64 * V;
-    __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH];
-    __shared__ ChainLds<V, NW> lds;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
-    uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
-    const int k = chunks > 1 ? chain_ticket<V, NW>(ws, col, lds) : 0;
-    const int c = min(col * WIDTH + lane * V, p.C - V);     // the lanes past the last channels do those again
-    const uint32_t off = (uint32_t)c * Elem<T>::kBytes;
-    const int t0 = (k * NW + wave) * TW;
-    Pack<T, V> xr[TW], rr[TW], ir[TW];
-#pragma unroll
-    for (int j = 0; j < TW; ++j) {
-        const long long t = min(t0 + j, p.T - 1);
-        xr[j] = load_pack<T, V>(static_cast<const T*>(p.x) + t * p.sx, off);
-        rr[j] = load_pack<T, V>(static_cast<const T*>(p.r) + t * p.sr, off);
-        ir[j] = load_pack<T, V>(static_cast<const T*>(p.i) + t * p.si, off);
-    }
-    const RowBits bits = row_bits<TW>(p, t0);
-    float decay[V], A[V], S[V], a[TW][V], u[TW][V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) { decay[v] = decay_of(p.lam[c + v], p.scale); A[v] = 1.0f; S[v] = 0.0f; }
-#pragma unroll
-    for (int j = 0; j < TW; ++j) {
+// The gates of a row's channels: y = log2 a, a, sigmoid(i) and b = sqrt(1 - a^2).
+struct Gates { float sr, a, si, b; };
+template <typename T, int V>
+__device__ __forceinline__ Gates gates(const Pack<T, V>& r, const Pack<T, V>& i, int v, float decay) {
+    Gates g;
+    g.sr = sigmoid(get<T, V>(r, v));
+    g.si = sigmoid(get<T, V>(i, v));
+    const float y = -decay * g.sr;
+    g.a = __builtin_amdgcn_exp2f(y);
+    g.b = __builtin_amdgcn_sqrtf(one_minus_square(y, g.a));
+    return g;
+}
+__device__ __forceinline__ bool bit(uint64_t m, int j) { return ((m >> j) & 1) != 0; }
+// a row's map on top of (A, S); `plain`: known to be neither a first row nor one of no sequence
+template <bool PLAIN, int V>
+__device__ __forceinline__ void add_row(const RecurArgs& p, const RowBits& bits, int j, int c, const float* a, float* u, float* A, float* S) {
+    if (!PLAIN && bit(bits.first, j)) {
+        const float* h0 = p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float y = -decay[v] * sigmoid(get<T, V>(rr[j], v)), e = __builtin_amdgcn_exp2f(y);
-            a[j][v] = e;
-            u[j][v] = __builtin_amdgcn_sqrtf(one_minus_square(y, e)) * sigmoid(get<T, V>(ir[j], v)) * get<T, V>(xr[j], v);
+            if (h0) u[v] = fmaf(a[v], h0[v], u[v]);
+            S[v] = u[v];
+            A[v] = kCut;
         }
-        if ((bits.first >> j) & 1) {
-            const float* h0 = p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+    } else if (!PLAIN && !bit(bits.inside, j)) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (h0) u[j][v] = fmaf(a[j][v], h0[v], u[j][v]);
-                S[v] = u[j][v];
-                A[v] = kCut;
-            }
-        } else if (!((bits.inside >> j) & 1)) {
+        for (int v = 0; v < V; ++v) { u[v] = S[v] = 0.0f; A[v] = kCut; }
+    } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) { u[j][v] = S[v] = 0.0f; A[v] = kCut; }
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                S[v] = fmaf(a[j][v], S[v], u[j][v]);
-                A[v] *= a[j][v];
-            }
+        for (int v = 0; v < V; ++v) {
+            S[v] = fmaf(a[v], S[v], u[v]);
+            A[v] *= a[v];
         }
     }
+}
+
+// ---- forward
+template <int V, int TW, bool PLAIN>
+__device__ __forceinline__ void add_rows(const RecurArgs& p, const RowBits& bits, int c, const float (*a)[V], float (*u)[V], float* A, float* S) {
+#pragma unroll
+    for (int j = 0; j < TW; ++j) add_row<PLAIN, V>(p, bits, j, c, a[j], u[j], A, S);
+}
+template <typename T, int V, int TW, bool PLAIN>
+__device__ __forceinline__ void fwd_rows(const RecurArgs& p, const RowBits& bits, int c, uint32_t off, const RowPointer& row, const float (*a)[V],
+                                         const float (*u)[V], float* h) {
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+        const bool cut = !PLAIN && (bit(bits.first, j) || !bit(bits.inside, j));
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = cut ? u[j][v] : fmaf(a[j][v], h[v], u[j][v]);
+        if (PLAIN || bit(bits.inside, j)) store_pack<T, V>(row.at, off + row.row(j), h);
+        if (!PLAIN && p.hT && bit(bits.last, j)) {
+            float* hT = p.hT + (size_t)bits.seq_of(j) * p.C + c;
+#pragma unroll
+            for (int v = 0; v < V; ++v) hT[v] = h[v];
+        }
+    }
+}
+
+template <typename T, int V, int TW, int NW>
+__global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, int chunks, int cols) {
+    constexpr int WIDTH = 64 * V, EB = Elem<T>::kBytes;
+    __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH];
+    __shared__ ChainLds<V> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
+    uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
+    const SeqSearch search(p);
+    const int k = chain_start<V>(p, ws, chunks, cols, col, lds);
+    const int c = min(col * WIDTH + lane * V, p.C - V);     // the lanes past the last channels do those again
+    const uint32_t off = (uint32_t)c * EB;
+    const int t0 = (k * NW + wave) * TW;
+    const RowBits bits = row_bits<TW>(p, search, t0);
+    Pack<T, V> xr[TW], rr[TW], ir[TW];
+    {
+        RowPointer px(p.x, p.sx, EB, t0, p.T), pr(p.r, p.sr, EB, t0, p.T), pi(p.i, p.si, EB, t0, p.T);
+#pragma unroll
+        for (int j = 0; j < TW; ++j) {
+            xr[j] = load_pack<T, V>(px.at, off + px.row_or_last(j));
+            rr[j] = load_pack<T, V>(pr.at, off + pr.row_or_last(j));
+            ir[j] = load_pack<T, V>(pi.at, off + pi.row_or_last(j));
+        }
+    }
+    float decay[V], A[V], S[V], h[V], a[TW][V], u[TW][V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) { decay[v] = lds.decay[lane * V + v]; A[v] = 1.0f; S[v] = h[v] = 0.0f; }
+#pragma unroll
+    for (int j = 0; j < TW; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Gates g = gates<T, V>(rr[j], ir[j], v, decay[v]);
+            a[j][v] = g.a;
+            u[j][v] = g.b * g.si * get<T, V>(xr[j], v);
+        }
+    if (bits.plain) add_rows<V, TW, true>(p, bits, c, a, u, A, S);
+    else add_rows<V, TW, false>(p, bits, c, a, u, A, S);
 #pragma unroll
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; }
     __syncthreads();
-    float h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = 0.0f;
     if (chunks > 1) {
 #pragma unroll
         for (int v = 0; v < V; ++v) { A[v] = 1.0f; S[v] = 0.0f; }
+#pragma unroll
         for (int w = 0; w < NW; ++w)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -301,102 +420,141 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
 #pragma unroll
         for (int v = 0; v < V; ++v) p.saved[(size_t)(t0 / kSavedRows) * p.C + c + v] = h[v];
     }
-#pragma unroll
-    for (int j = 0; j < TW; ++j) {
-        const bool cut = (((bits.first | ~bits.inside) >> j) & 1) != 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = cut ? u[j][v] : fmaf(a[j][v], h[v], u[j][v]);
-        if ((bits.inside >> j) & 1) store_pack<T, V>(static_cast<T*>(p.h) + (long long)(t0 + j) * p.sh, off, h);
-        if (p.hT && ((bits.last >> j) & 1)) {
-            float* hT = p.hT + (size_t)bits.seq_of(j) * p.C + c;
-#pragma unroll
-            for (int v = 0; v < V; ++v) hT[v] = h[v];
-        }
-    }
+    const RowPointer ph(p.h, p.sh, EB, t0, p.T);
+    if (bits.plain) fwd_rows<T, V, TW, true>(p, bits, c, off, ph, a, u, h);
+    else fwd_rows<T, V, TW, false>(p, bits, c, off, ph, a, u, h);
     if (p.hT) pass_empty<V>(p, p.h0, p.hT, c, (long long)k * NW + wave, (long long)chunks * NW);
 }
 
 // ---- backward
-template <typename T, int V, int TW, int NW>
-__global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, float* parts, int chunks, int cols) {
-    constexpr int WIDTH = 64 * V;
-    __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH], mapD[NW][WIDTH];
-    __shared__ ChainLds<V, NW> lds;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
-    uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
-    const int n = chunks > 1 ? chain_ticket<V, NW>(ws, col, lds) : 0, k = chunks - 1 - n;   // the chain runs from the last chunk
-    const int c = min(col * WIDTH + lane * V, p.C - V);
-    const uint32_t off = (uint32_t)c * Elem<T>::kBytes;
-    const int t0 = (k * NW + wave) * TW;
-    Pack<T, V> xr[TW], rr[TW], ir[TW], dr[TW];
-#pragma unroll
-    for (int j = 0; j < TW; ++j) {
-        const long long t = min(t0 + j, p.T - 1);
-        xr[j] = load_pack<T, V>(static_cast<const T*>(p.x) + t * p.sx, off);
-        rr[j] = load_pack<T, V>(static_cast<const T*>(p.r) + t * p.sr, off);
-        ir[j] = load_pack<T, V>(static_cast<const T*>(p.i) + t * p.si, off);
-        dr[j] = load_pack<T, V>(static_cast<const T*>(p.dh) + t * p.sdh, off);
-    }
-    const RowBits bits = row_bits<TW>(p, t0);
-    float decay[V], A[V], S[V], D[V], h[V], a[TW][V], u[TW][V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        decay[v] = decay_of(p.lam[c + v], p.scale);
-        h[v] = p.saved[(size_t)k * p.C + c + v];
-        A[v] = 1.0f; S[v] = 0.0f; D[v] = 0.0f;
-    }
-#pragma unroll
-    for (int j = 0; j < TW; ++j) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float y = -decay[v] * sigmoid(get<T, V>(rr[j], v)), e = __builtin_amdgcn_exp2f(y);
-            a[j][v] = e;
-            u[j][v] = __builtin_amdgcn_sqrtf(one_minus_square(y, e)) * sigmoid(get<T, V>(ir[j], v)) * get<T, V>(xr[j], v);
-        }
-        if ((bits.first >> j) & 1) {
-            const float* h0 = p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (h0) u[j][v] = fmaf(a[j][v], h0[v], u[j][v]);
-                S[v] = u[j][v];
-                A[v] = kCut;
-            }
-        } else if (!((bits.inside >> j) & 1)) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) { u[j][v] = S[v] = 0.0f; A[v] = kCut; }
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                S[v] = fmaf(a[j][v], S[v], u[j][v]);
-                A[v] *= a[j][v];
-            }
-        }
-    }
-    // e in front of the rows from the one behind them: D + A e
-    auto grad = [&](int j, int v) { return get<T, V>(dr[j], v); };
+// The rows' maps and what the second run needs: u gives way to the state in front of each row there.
+template <typename T, int V, int TW>
+struct BwdRows {
+    Pack<T, V> x[TW], dh[TW];
+    float a[TW][V], u[TW][V], sr[TW][V], si[TW][V], b[TW][V];
+};
+template <typename T, int V, int TW, bool PLAIN>
+__device__ __forceinline__ void bwd_maps(const RecurArgs& p, const RowBits& bits, int c, BwdRows<T, V, TW>& w, float* A, float* S, float* D) {
+    add_rows<V, TW, PLAIN>(p, bits, c, w.a, w.u, A, S);
+    // e in front of the rows from the one behind them: D + A e.  Behind a sequence's last row there is another's first, whose e
+    // does not come here, or a row of none: D is 0 there.
 #pragma unroll
     for (int j = TW - 1; j >= 0; --j) {
-        if (!((bits.inside >> j) & 1) || ((bits.first >> j) & 1)) {
+        if (!PLAIN && (bit(bits.first, j) || !bit(bits.inside, j))) {
 #pragma unroll
             for (int v = 0; v < V; ++v) D[v] = 0.0f;
         } else {
-            const float* dT = p.dhT && ((bits.last >> j) & 1) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+            const float* dT = !PLAIN && p.dhT && bit(bits.last, j) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                // behind a sequence's last row there is another's first, whose e does not come here: D is 0 there
-                D[v] = a[j][v] * (grad(j, v) + D[v] + (dT ? dT[v] : 0.0f));
-            }
+            for (int v = 0; v < V; ++v) D[v] = w.a[j][v] * (get<T, V>(w.dh[j], v) + D[v] + (dT ? dT[v] : 0.0f));
         }
     }
+}
+template <typename T, int V, int TW, bool PLAIN>
+__device__ __forceinline__ void bwd_rows(const RecurArgs& p, const RowBits& bits, int t0, int c, uint32_t off, const float* decay, BwdRows<T, V, TW>& w,
+                                         float* h, float* e, float* sum) {
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+        const bool first = !PLAIN && bit(bits.first, j), cut = first || (!PLAIN && !bit(bits.inside, j));
+        const float* h0 = first && p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float next = cut ? w.u[j][v] : fmaf(w.a[j][v], h[v], w.u[j][v]);
+            w.u[j][v] = cut ? (h0 ? h0[v] : 0.0f) : h[v];
+            h[v] = next;
+        }
+    }
+    constexpr int EB = Elem<T>::kBytes;
+    const RowPointer px(p.dx, p.sdx, EB, t0, p.T), pr(p.dr, p.sdr, EB, t0, p.T), pi(p.di, p.sdi, EB, t0, p.T);
+    float log2a[V];                                         // of an open gate, in natural logarithms
+#pragma unroll
+    for (int v = 0; v < V; ++v) log2a[v] = -decay[v] * 0.6931471805599453f;
+#pragma unroll
+    for (int j = TW - 1; j >= 0; --j) {
+        if (PLAIN || bit(bits.inside, j)) {
+            const float* dT = !PLAIN && p.dhT && bit(bits.last, j) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+            float dx[V], di[V], dr[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float a = w.a[j][v], b = w.b[j][v], si = w.si[j][v], sr = w.sr[j][v], x = get<T, V>(w.x[j], v);
+                const float ib = b > 0.0f ? __builtin_amdgcn_rcpf(b) : 0.0f;
+                const float g = get<T, V>(w.dh[j], v) + e[v] + (dT ? dT[v] : 0.0f), gs = g * si;
+                e[v] = a * g;
+                const float q = log2a[v] * sr * fmaf(e[v], w.u[j][v], -(a * ib) * (a * gs * x));
+                sum[v] += q;
+                dx[v] = b * gs;
+                di[v] = dx[v] * x * (1.0f - si);
+                dr[v] = q * (1.0f - sr);
+            }
+            store_pack<T, V>(px.at, off + px.row(j), dx);
+            store_pack<T, V>(pi.at, off + pi.row(j), di);
+            store_pack<T, V>(pr.at, off + pr.row(j), dr);
+        }
+        if (!PLAIN && bit(bits.first, j) && p.dh0) {
+            float* d0 = p.dh0 + (size_t)bits.seq_of(j) * p.C + c;
+#pragma unroll
+            for (int v = 0; v < V; ++v) d0[v] = e[v];
+        }
+        if (!PLAIN && (bit(bits.first, j) || !bit(bits.inside, j))) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) e[v] = 0.0f;
+        }
+    }
+}
+
+template <typename T, int V, int TW, int NW>
+__global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, float* parts, int chunks, int cols) {
+    constexpr int WIDTH = 64 * V, EB = Elem<T>::kBytes;
+    __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH], mapD[NW][WIDTH];
+    __shared__ ChainLds<V> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
+    uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
+    const SeqSearch search(p);
+    const int n = chain_start<V>(p, ws, chunks, cols, col, lds), k = chunks - 1 - n;   // the chain runs from the last chunk
+    const int c = min(col * WIDTH + lane * V, p.C - V);
+    const uint32_t off = (uint32_t)c * EB;
+    const int t0 = (k * NW + wave) * TW;
+    const RowBits bits = row_bits<TW>(p, search, t0);
+    BwdRows<T, V, TW> rows;
+    Pack<T, V> rr[TW], ir[TW];
+    {
+        RowPointer px(p.x, p.sx, EB, t0, p.T), pr(p.r, p.sr, EB, t0, p.T), pi(p.i, p.si, EB, t0, p.T), pd(p.dh, p.sdh, EB, t0, p.T);
+#pragma unroll
+        for (int j = 0; j < TW; ++j) {
+            rr[j] = load_pack<T, V>(pr.at, off + pr.row_or_last(j));
+            ir[j] = load_pack<T, V>(pi.at, off + pi.row_or_last(j));
+            rows.x[j] = load_pack<T, V>(px.at, off + px.row_or_last(j));
+        }
+#pragma unroll
+        for (int j = 0; j < TW; ++j) {
+            rows.dh[j] = load_pack<T, V>(pd.at, off + pd.row_or_last(j));
+        }
+    }
+    float decay[V], A[V], S[V], D[V], h[V], e[V], sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        decay[v] = lds.decay[lane * V + v];
+        h[v] = p.saved[(size_t)k * p.C + c + v];
+        A[v] = 1.0f;
+        S[v] = D[v] = e[v] = sum[v] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < TW; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Gates g = gates<T, V>(rr[j], ir[j], v, decay[v]);
+            rows.a[j][v] = g.a; rows.sr[j][v] = g.sr; rows.si[j][v] = g.si; rows.b[j][v] = g.b;
+            rows.u[j][v] = g.b * g.si * get<T, V>(rows.x[j], v);
+        }
+    if (bits.plain) bwd_maps<T, V, TW, true>(p, bits, c, rows, A, S, D);
+    else bwd_maps<T, V, TW, false>(p, bits, c, rows, A, S, D);
 #pragma unroll
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; mapD[wave][lane * V + v] = D[v]; }
     __syncthreads();
-    float e[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) e[v] = 0.0f;
     if (chunks > 1) {
 #pragma unroll
         for (int v = 0; v < V; ++v) { A[v] = 1.0f; D[v] = 0.0f; }
+#pragma unroll
         for (int w = NW - 1; w >= 0; --w)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -411,57 +569,8 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
     for (int w = 0; w < wave; ++w)
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(mapA[w][lane * V + v], h[v], mapS[w][lane * V + v]);
-    // the state in front of each row takes the place of its u
-#pragma unroll
-    for (int j = 0; j < TW; ++j) {
-        const bool cut = ((bits.first >> j) & 1) || !((bits.inside >> j) & 1);
-        const float* h0 = cut && p.h0 && ((bits.first >> j) & 1) ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float next = cut ? u[j][v] : fmaf(a[j][v], h[v], u[j][v]);
-            u[j][v] = cut ? (h0 ? h0[v] : 0.0f) : h[v];
-            h[v] = next;
-        }
-    }
-    float sum[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] = 0.0f;
-#pragma unroll
-    for (int j = TW - 1; j >= 0; --j) {
-        if (!((bits.inside >> j) & 1)) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) e[v] = 0.0f;
-            continue;
-        }
-        const float* dT = p.dhT && ((bits.last >> j) & 1) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
-        float dx[V], di[V], dg[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float sr = sigmoid(get<T, V>(rr[j], v)), si = sigmoid(get<T, V>(ir[j], v)), x = get<T, V>(xr[j], v);
-            const float y = -decay[v] * sr, av = a[j][v], b2 = one_minus_square(y, av);
-            const float ib = b2 > 1.2e-38f ? __builtin_amdgcn_rsqf(b2) : 0.0f, b = b2 * ib;
-            const float g = grad(j, v) + e[v] + (dT ? dT[v] : 0.0f);
-            e[v] = av * g;
-            const float gs = g * si, q = y * 0.6931471805599453f * (e[v] * u[j][v] - av * av * ib * gs * x);
-            sum[v] += q;
-            dx[v] = b * gs;
-            di[v] = dx[v] * x * (1.0f - si);
-            dg[v] = q * (1.0f - sr);
-        }
-        const long long t = t0 + j;
-        store_pack<T, V>(static_cast<T*>(p.dx) + t * p.sdx, off, dx);
-        store_pack<T, V>(static_cast<T*>(p.di) + t * p.sdi, off, di);
-        store_pack<T, V>(static_cast<T*>(p.dr) + t * p.sdr, off, dg);
-        if ((bits.first >> j) & 1) {
-            if (p.dh0) {
-                float* d0 = p.dh0 + (size_t)bits.seq_of(j) * p.C + c;
-#pragma unroll
-                for (int v = 0; v < V; ++v) d0[v] = e[v];
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) e[v] = 0.0f;
-        }
-    }
+    if (bits.plain) bwd_rows<T, V, TW, true>(p, bits, t0, c, off, decay, rows, h, e, sum);
+    else bwd_rows<T, V, TW, false>(p, bits, t0, c, off, decay, rows, h, e, sum);
     if (p.dh0) pass_empty<V>(p, p.dhT, p.dh0, c, (long long)k * NW + wave, (long long)chunks * NW);
     __syncthreads();                                        // the maps have been read
 #pragma unroll
@@ -519,12 +628,12 @@ __global__ __launch_bounds__(256) void recur_step_kernel(const RecurArgs p, floa
     float h = state[(size_t)slot * p.C + c];
     for (int t = row; t < (slots ? p.T : row + 1); ++t) {
         if (slots && slots[t] != slot) continue;
-        const float x = get<T, 1>(load_pack<T, 1>(static_cast<const T*>(p.x) + t * p.sx, off), 0);
-        const float r = get<T, 1>(load_pack<T, 1>(static_cast<const T*>(p.r) + t * p.sr, off), 0);
-        const float i = get<T, 1>(load_pack<T, 1>(static_cast<const T*>(p.i) + t * p.si, off), 0);
-        const float y = -decay * sigmoid(r), a = __builtin_amdgcn_exp2f(y);
-        h = fmaf(a, h, __builtin_amdgcn_sqrtf(one_minus_square(y, a)) * sigmoid(i) * x);
-        store_pack<T, 1>(static_cast<T*>(p.h) + t * p.sh, off, &h);
+        const uint64_t EB = Elem<T>::kBytes;
+        const Pack<T, 1> x = load_pack<T, 1>((uint64_t)p.x + t * p.sx * EB, off), r = load_pack<T, 1>((uint64_t)p.r + t * p.sr * EB, off),
+                         i = load_pack<T, 1>((uint64_t)p.i + t * p.si * EB, off);
+        const Gates g = gates<T, 1>(r, i, 0, decay);
+        h = fmaf(g.a, h, g.b * g.si * get<T, 1>(x, 0));
+        store_pack<T, 1>((uint64_t)p.h + t * p.sh * EB, off, &h);
     }
     state[(size_t)slot * p.C + c] = h;
 }
