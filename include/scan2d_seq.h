@@ -108,7 +108,7 @@ size_t scan2d_seq_recur_workspace_bytes(const scan2d_recur_desc* desc, int pass)
 enum { SCAN2D_ACT_NONE = 0, SCAN2D_ACT_SILU = 1, SCAN2D_ACT_GELU = 2 };
 typedef struct {
     int32_t  N, C, G;          /* items, channels, groups: >= 1, C a multiple of G; C < 2^24 */
-    int64_t  P;                /* positions per item, >= 1; N * P < 2^31 */
+    int64_t  P;                /* positions per item, >= 1; N * P < 2^31 - 4096 */
     int32_t  dtype;            /* SCAN2D_F32 or SCAN2D_BF16: type of x, y, dy, dx */
     int32_t  act;
     float    eps;              /* >= 0 */

@@ -6,10 +6,14 @@
 //
 // Held form (group_norm_fwd_kernel, group_norm_bwd_kernel): a team of lanes holds all positions of an item's slab in
 // registers as they were loaded: one read.  Teams are a power of two of lanes within a wavefront (nothing waits for another
-// wavefront; a single token's groups, small maps), or a workgroup.  A team goes on to the next item of its slab with its
-// channels' parameters, and in the backward pass its channels' sums, in registers.
-// Split form, where an item's slab does not fit: one kernel takes the mean and the squared deviations from it of tiles held in registers,
-// one joins the tiles of an item (M2 = sum M2_i + sum n_i (mean_i - mean)^2), one reads the tensor again and writes.
+// wavefront; a single token's groups, small maps), or a workgroup.  A team goes on to the next items of its slab with its
+// channels' parameters, and in the backward pass its channels' sums, in registers; where an item is one row of a lane, it takes
+// several items at once, so that enough bytes are on their way.
+// Split form, where an item's slab does not fit: a workgroup has a tile, a share of an item's positions, and goes through it kRows rows
+// of a lane at a time.  Forward: each lane keeps mean and squared deviations of its channels (rows in registers: their mean, the deviations
+// from it, joined to those before by M2 = M2_1 + M2_2 + n1 n2 / (n1 + n2) (mean_1 - mean_2)^2), which are joined to those of the tile, those
+// of the tiles to the item's; then the tensor is read again and written, last rows first, which are the ones still in a cache.
+// Backward: the channels' sums of dv and dv xh of a tile, joined to those of the item and with gamma to the groups', then dx from a second read.
 // The variance is always taken from deviations, never from the difference of two large sums.
 // All sums run in a fixed order.
 #include "scan2d_seq.hpp"
@@ -74,19 +78,23 @@ struct Geo {
     int tpg;                             // lanes that add up a group, a power of two
 };
 
-// A team's slab, and this lane's channels of it.
-template <int V>
+// A team's slab, and this lane's channels of it.  ONE: a lane's channels are of one group (V divides the groups' channels).
+template <int V, bool ONE>
 struct Lane {
+    static constexpr int GV = ONE ? 1 : V;                 // values per group of a lane's channels
     int lt;                              // within the team
     int slot, c;                         // which of the team's rows; first channel
-    int lo, hi;                          // the slab's channels
+    int lo, width;                       // the slab's channels
     int groups, D;                       // the slab's groups, their channels (of the slab)
     int g0;                              // its first group
+    int first;                           // the lane's first own channel within the slab
+    int gr[GV];                          // the group, within the slab, of each channel
     bool on;                             // has a row at all
     bool own[V];                         // which channels are this lane's
     bool all;
     __device__ Lane(const Geo& q, int C, int G, int slab, int lane) {
         lt = lane;
+        int hi;
         if (q.spg > 1) {
             g0 = slab / q.spg;
             const int Dg = C / G, part = slab % q.spg;
@@ -101,18 +109,21 @@ struct Lane {
             lo = g0 * D;
             hi = lo + groups * D;
         }
+        width = hi - lo;
         slot = lane / q.lanes;
-        const int first = lo + (lane % q.lanes) * V;
-        on = slot < q.slots && first < hi;
-        c = min(first, C - V);
+        const int mine = lo + (lane % q.lanes) * V;
+        first = mine - lo;
+        on = slot < q.slots && mine < hi;
+        c = min(mine, C - V);
         all = true;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            own[v] = on && c + v >= first && c + v < hi;
+            own[v] = on && c + v >= mine && c + v < hi;
             all = all && own[v];
         }
+#pragma unroll
+        for (int v = 0; v < GV; ++v) gr[v] = min(max((ONE ? mine : c + v) - lo, 0) / D, groups - 1);
     }
-    __device__ __forceinline__ int group_of(int v) const { return min(max((c + v - lo) / D, 0), groups - 1); }
 };
 
 template <bool WAVE>
@@ -127,27 +138,40 @@ __device__ __forceinline__ void team_sync() {
 }
 
 // Sums of NR values over a team's rows and the channels of each group of its slab: done(group, sums) is called by one lane of each
-// group.  The values of channels that are not the lane's are not looked at.  red: NR x (ts V) floats of the team.
-template <int V, int NR, bool WAVE, typename Done>
-__device__ __forceinline__ void group_sums(const Geo& q, const Lane<V>& l, float* red, const float (&val)[NR][V], Done done) {
-    const int width = l.hi - l.lo, size = q.ts * V;
+// group.  The values of channels that are not the lane's are not looked at.  red: NR x size floats of the team, size at least
+// ts V (ts where a lane's channels are of one group and added up first).
+template <int V, bool ONE, int NR, bool WAVE, typename Done>
+__device__ __forceinline__ void group_sums(const Geo& q, const Lane<V, ONE>& l, float* red, int size, const float (&val)[NR][V], Done done) {
+    const int width = ONE ? q.lanes : l.width, D = ONE ? (l.D + V - 1) / V : l.D;
+    if constexpr (ONE) {
+        if (l.on) {
 #pragma unroll
-    for (int r = 0; r < NR; ++r)
+            for (int r = 0; r < NR; ++r) {
+                float s = l.own[0] ? val[r][0] : 0.0f;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (l.own[v]) red[r * size + l.slot * width + l.c + v - l.lo] = val[r][v];
+                for (int v = 1; v < V; ++v) s += l.own[v] ? val[r][v] : 0.0f;
+                red[r * size + l.lt] = s;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (l.own[v]) red[r * size + l.slot * width + l.c + v - l.lo] = val[r][v];
+    }
     team_sync<WAVE>();
-    const int qq = l.lt & (q.tpg - 1), n = q.slots * l.D, row0 = qq / l.D, d0 = qq % l.D, rowstep = q.tpg / l.D, dstep = q.tpg % l.D;
+    const int qq = l.lt & (q.tpg - 1), n = q.slots * D, row0 = qq / D, d0 = qq % D, rowstep = q.tpg / D, dstep = q.tpg % D;
     for (int g = l.lt / q.tpg; g < l.groups; g += q.ts / q.tpg) {
         float s[NR];
 #pragma unroll
         for (int r = 0; r < NR; ++r) s[r] = 0.0f;
         for (int e = qq, row = row0, d = d0; e < n; e += q.tpg) {
 #pragma unroll
-            for (int r = 0; r < NR; ++r) s[r] += red[r * size + row * width + g * l.D + d];
+            for (int r = 0; r < NR; ++r) s[r] += red[r * size + row * width + g * D + d];
             row += rowstep;
             d += dstep;
-            if (d >= l.D) { d -= l.D; ++row; }
+            if (d >= D) { d -= D; ++row; }
         }
         for (int m = 1; m < q.tpg; m <<= 1)
 #pragma unroll
@@ -175,8 +199,8 @@ __device__ __forceinline__ void load_params(const GroupNormArgs& p, int c, float
         beta[v] = p.beta ? p.beta[c + v] : 0.0f;
     }
 }
-template <typename T, int V>
-__device__ __forceinline__ void store_own(T* p, const Lane<V>& l, const float* v) {
+template <typename T, int V, bool ONE>
+__device__ __forceinline__ void store_own(T* p, const Lane<V, ONE>& l, const float* v) {
     if (l.all) {
         store_pack<T, V>(p, v);
     } else {
@@ -186,459 +210,561 @@ __device__ __forceinline__ void store_own(T* p, const Lane<V>& l, const float* v
     }
 }
 
-// ---- held form
-template <typename T, int V, int K, int TH, bool WAVE, int ACT>
+// ---- held form.  R items at once, K rows of each per lane.
+template <typename T, int V, bool ONE, int K, int R, int TH, bool WAVE, int ACT>
 __global__ __launch_bounds__(TH) void group_norm_fwd_kernel(const GroupNormArgs p, const Geo q, int teams) {
-    __shared__ float red[TH * V], res[2][TH * V];
+    constexpr int GV = Lane<V, ONE>::GV, PER = ONE ? 1 : V;                  // floats of red per lane
+    __shared__ float red[R * TH * PER], res[2][R][TH * GV];
     __shared__ int cnts[WAVE ? TH : 1];
     const int tid = threadIdx.x, lt = WAVE ? tid & (q.ts - 1) : tid, base = tid - lt;
     const int team = WAVE ? (int)((blockIdx.x * (long long)TH + tid) / q.ts) : (int)blockIdx.x;      // teams is a multiple of slabs
-    const Lane<V> l(q, p.C, p.G, team % q.slabs, lt);
-    float* const myred = red + base * V;
-    float *const mean_of = res[0] + base * V, *const rstd_of = res[1] + base * V;
+    const Lane<V, ONE> l(q, p.C, p.G, team % q.slabs, lt);
+    float* const myred = red + R * base * PER;
     float gamma[V], beta[V];
     load_params<V>(p, l.c, gamma, beta);
-    int gr[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) gr[v] = l.group_of(v);
-    const int step = teams / q.slabs, rounds = (p.N + step - 1) / step;
+    const int step = teams / q.slabs, rounds = (p.N + step * R - 1) / (step * R);
     for (int it = 0; it < rounds; ++it) {
-        const long long n = team / q.slabs + (long long)it * step;
-        const bool real = n < p.N && team < teams;      // the last workgroup may have lanes to spare
-        const long long row0 = (real ? n : 0) * p.P;
-        Pack<T, V> x[K];
-        bool live[K];
-        int mine = 0;
+        Pack<T, V> x[R][K];
+        bool live[R][K];
+        long long item[R], row0[R];
+        int rows[R];
+        bool real[R];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int r = l.slot + k * q.slots;
-            const long long row = row0 + min(r, p.P - 1);
-            x[k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
-            live[k] = real && l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
-            mine += live[k];
-        }
-        int rows = p.P;
-        if (p.mask != nullptr) rows = count_rows<WAVE>(&cnts[base], lt, lt % q.lanes == 0, mine);
-        const float M = (float)rows * (float)l.D, inv = rows > 0 ? 1.0f / M : 0.0f;
-        float s[1][V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            s[0][v] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < K; ++k) s[0][v] += live[k] ? get<T, V>(x[k], v) : 0.0f;
-        }
-        group_sums<V, 1, WAVE>(q, l, myred, s, [&](int g, const float* t) { mean_of[g] = t[0] * inv; });
-        float mean[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            mean[v] = mean_of[gr[v]];
-            s[0][v] = 0.0f;
+        for (int i = 0; i < R; ++i) {
+            const long long n = team / q.slabs + ((long long)it * R + i) * step;
+            real[i] = n < p.N && team < teams;              // the last workgroup may have lanes to spare
+            item[i] = n;
+            row0[i] = (real[i] ? n : 0) * p.P;
+            int mine = 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const float d = live[k] ? get<T, V>(x[k], v) - mean[v] : 0.0f;
-                s[0][v] = fmaf(d, d, s[0][v]);
+                const int r = l.slot + k * q.slots;
+                const long long row = row0[i] + min(r, p.P - 1);
+                x[i][k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
+                live[i][k] = real[i] && l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
+                mine += live[i][k];
+            }
+            rows[i] = p.P;
+            if (p.mask != nullptr) rows[i] = count_rows<WAVE>(&cnts[base], lt, lt % q.lanes == 0, mine);
+        }
+        float s[R][V], mean[R][GV], rstd[R][GV];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                s[i][v] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < K; ++k) s[i][v] += live[i][k] ? get<T, V>(x[i][k], v) : 0.0f;
+            }
+        float inv[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) inv[i] = rows[i] > 0 ? 1.0f / ((float)rows[i] * (float)l.D) : 0.0f;
+        group_sums<V, ONE, R, WAVE>(q, l, myred, q.ts * PER, s, [&](int g, const float* t) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) res[0][i][base * GV + g] = t[i] * inv[i];
+        });
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+#pragma unroll
+            for (int v = 0; v < GV; ++v) mean[i][v] = res[0][i][base * GV + l.gr[v]];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                s[i][v] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const float d = live[i][k] ? get<T, V>(x[i][k], v) - mean[i][ONE ? 0 : v] : 0.0f;
+                    s[i][v] = fmaf(d, d, s[i][v]);
+                }
             }
         }
-        group_sums<V, 1, WAVE>(q, l, myred, s, [&](int g, const float* t) {
-            const float rstd = rows > 0 ? 1.0f / sqrtf(t[0] * inv + p.eps) : 0.0f;
-            rstd_of[g] = rstd;
-            if (real) {
-                float* st = p.stats + ((size_t)n * p.G + l.g0 + g) * 2;
-                st[0] = mean_of[g];
-                st[1] = rstd;
+        group_sums<V, ONE, R, WAVE>(q, l, myred, q.ts * PER, s, [&](int g, const float* t) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float rs = rows[i] > 0 ? 1.0f / sqrtf(t[i] * inv[i] + p.eps) : 0.0f;
+                res[1][i][base * GV + g] = rs;
+                if (real[i]) {
+                    float* st = p.stats + ((size_t)item[i] * p.G + l.g0 + g) * 2;
+                    st[0] = res[0][i][base * GV + g];
+                    st[1] = rs;
+                }
             }
         });
-        float rstd[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) rstd[v] = rstd_of[gr[v]];
+        for (int i = 0; i < R; ++i) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int r = l.slot + k * q.slots;
-            if (real && l.on && r < p.P) {
-                float y[V];
+            for (int v = 0; v < GV; ++v) rstd[i][v] = res[1][i][base * GV + l.gr[v]];
 #pragma unroll
-                for (int v = 0; v < V; ++v) y[v] = live[k] ? act_of<ACT>(fmaf((get<T, V>(x[k], v) - mean[v]) * rstd[v], gamma[v], beta[v])) : 0.0f;
-                store_own<T, V>(static_cast<T*>(p.y) + (row0 + r) * p.sy + l.c, l, y);
+            for (int k = 0; k < K; ++k) {
+                const int r = l.slot + k * q.slots;
+                if (real[i] && l.on && r < p.P) {
+                    float y[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        y[v] = live[i][k] ? act_of<ACT>(fmaf((get<T, V>(x[i][k], v) - mean[i][ONE ? 0 : v]) * rstd[i][ONE ? 0 : v], gamma[v], beta[v])) : 0.0f;
+                    store_own<T, V>(static_cast<T*>(p.y) + (row0[i] + r) * p.sy + l.c, l, y);
+                }
             }
         }
     }
 }
 
 // parts: [..][C][2], the sums for dbeta and dgamma of the items that a team, or a workgroup of teams, had.
-template <typename T, int V, int K, int TH, bool WAVE, int ACT>
+template <typename T, int V, bool ONE, int K, int R, int TH, bool WAVE, int ACT>
 __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs p, const Geo q, int teams, float2* parts) {
-    __shared__ float red[2 * TH * V], res[2][TH * V];
+    constexpr int GV = Lane<V, ONE>::GV, PER = ONE ? 1 : V;
+    constexpr int RED = 2 * R * TH * PER > 2 * TH * V ? 2 * R * TH * PER : 2 * TH * V;       // the channels' sums at the end use it too
+    __shared__ float red[RED], res[2][R][TH * GV];
     __shared__ int cnts[WAVE ? TH : 1];
     const int tid = threadIdx.x, lt = WAVE ? tid & (q.ts - 1) : tid, base = tid - lt;
     const int team = WAVE ? (int)((blockIdx.x * (long long)TH + tid) / q.ts) : (int)blockIdx.x;
-    const Lane<V> l(q, p.C, p.G, team % q.slabs, lt);
-    float* const myred = red + 2 * base * V;
-    float *const s1_of = res[0] + base * V, *const s2_of = res[1] + base * V;
+    const Lane<V, ONE> l(q, p.C, p.G, team % q.slabs, lt);
+    float* const myred = red + 2 * R * base * PER;
     float gamma[V], beta[V], accb[V], accg[V];
     load_params<V>(p, l.c, gamma, beta);
-    int gr[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) { gr[v] = l.group_of(v); accb[v] = accg[v] = 0.0f; }
-    const int step = teams / q.slabs, rounds = (p.N + step - 1) / step;
+    for (int v = 0; v < V; ++v) accb[v] = accg[v] = 0.0f;
+    const int step = teams / q.slabs, rounds = (p.N + step * R - 1) / (step * R);
     for (int it = 0; it < rounds; ++it) {
-        const long long n = team / q.slabs + (long long)it * step;
-        const bool real = n < p.N && team < teams;      // the last workgroup may have lanes to spare
-        const long long row0 = (real ? n : 0) * p.P;
-        Pack<T, V> x[K], dy[K];
-        bool live[K];
-        int mine = 0;
+        Pack<T, V> x[R][K], dy[R][K];
+        bool live[R][K], real[R];
+        long long row0[R];
+        int rows[R];
+        float mean[R][GV], rstd[R][GV];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int r = l.slot + k * q.slots;
-            const long long row = row0 + min(r, p.P - 1);
-            x[k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
-            dy[k] = load_pack<T, V>(static_cast<const T*>(p.dy) + row * p.sdy + l.c);
-            live[k] = real && l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
-            mine += live[k];
-        }
-        float mean[V], rstd[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float* st = p.stats + ((size_t)(real ? n : 0) * p.G + l.g0 + gr[v]) * 2;
-            mean[v] = st[0];
-            rstd[v] = st[1];
-        }
-        int rows = p.P;
-        if (p.mask != nullptr) rows = count_rows<WAVE>(&cnts[base], lt, lt % q.lanes == 0, mine);
-        const float inv = rows > 0 ? 1.0f / ((float)rows * (float)l.D) : 0.0f;
-        float s[2][V], dv[K][V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float b = 0.0f, g = 0.0f;
+        for (int i = 0; i < R; ++i) {
+            const long long n = team / q.slabs + ((long long)it * R + i) * step;
+            real[i] = n < p.N && team < teams;
+            row0[i] = (real[i] ? n : 0) * p.P;
+            int mine = 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const float xh = (get<T, V>(x[k], v) - mean[v]) * rstd[v];
-                dv[k][v] = live[k] ? get<T, V>(dy[k], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v])) : 0.0f;
-                b += dv[k][v];
-                g += live[k] ? dv[k][v] * xh : 0.0f;
+                const int r = l.slot + k * q.slots;
+                const long long row = row0[i] + min(r, p.P - 1);
+                x[i][k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
+                dy[i][k] = load_pack<T, V>(static_cast<const T*>(p.dy) + row * p.sdy + l.c);
+                live[i][k] = real[i] && l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
+                mine += live[i][k];
             }
-            accb[v] += b;
-            accg[v] += g;
-            s[0][v] = b * gamma[v];
-            s[1][v] = g * gamma[v];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) {
+                const float* st = p.stats + ((size_t)(real[i] ? n : 0) * p.G + l.g0 + l.gr[v]) * 2;
+                mean[i][v] = st[0];
+                rstd[i][v] = st[1];
+            }
+            rows[i] = p.P;
+            if (p.mask != nullptr) rows[i] = count_rows<WAVE>(&cnts[base], lt, lt % q.lanes == 0, mine);
         }
-        group_sums<V, 2, WAVE>(q, l, myred, s, [&](int g, const float* t) { s1_of[g] = t[0] * inv; s2_of[g] = t[1] * inv; });
-        float s1[V], s2[V];
+        float s[2 * R][V], dv[R][K][V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) { s1[v] = s1_of[gr[v]]; s2[v] = s2_of[gr[v]]; }
+        for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int r = l.slot + k * q.slots;
-            if (real && l.on && r < p.P) {
-                float dx[V];
+            for (int v = 0; v < V; ++v) {
+                float b = 0.0f, g = 0.0f;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float xh = (get<T, V>(x[k], v) - mean[v]) * rstd[v];
-                    dx[v] = live[k] ? rstd[v] * (fmaf(dv[k][v], gamma[v], -s1[v]) - xh * s2[v]) : 0.0f;
+                for (int k = 0; k < K; ++k) {
+                    const float xh = (get<T, V>(x[i][k], v) - mean[i][ONE ? 0 : v]) * rstd[i][ONE ? 0 : v];
+                    dv[i][k][v] = live[i][k] ? get<T, V>(dy[i][k], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v])) : 0.0f;
+                    b += dv[i][k][v];
+                    g += live[i][k] ? dv[i][k][v] * xh : 0.0f;
                 }
-                store_own<T, V>(static_cast<T*>(p.dx) + (row0 + r) * p.sdx + l.c, l, dx);
+                accb[v] += b;
+                accg[v] += g;
+                s[2 * i][v] = b * gamma[v];
+                s[2 * i + 1][v] = g * gamma[v];
+            }
+        group_sums<V, ONE, 2 * R, WAVE>(q, l, myred, q.ts * PER, s, [&](int g, const float* t) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float inv = rows[i] > 0 ? 1.0f / ((float)rows[i] * (float)l.D) : 0.0f;
+                res[0][i][base * GV + g] = t[2 * i] * inv;
+                res[1][i][base * GV + g] = t[2 * i + 1] * inv;
+            }
+        });
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            float s1[GV], s2[GV];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) { s1[v] = res[0][i][base * GV + l.gr[v]]; s2[v] = res[1][i][base * GV + l.gr[v]]; }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int r = l.slot + k * q.slots;
+                if (real[i] && l.on && r < p.P) {
+                    float dx[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const int w = ONE ? 0 : v;
+                        const float xh = (get<T, V>(x[i][k], v) - mean[i][w]) * rstd[i][w];
+                        dx[v] = live[i][k] ? rstd[i][w] * (fmaf(dv[i][k][v], gamma[v], -s1[w]) - xh * s2[w]) : 0.0f;
+                    }
+                    store_own<T, V>(static_cast<T*>(p.dx) + (row0[i] + r) * p.sdx + l.c, l, dx);
+                }
             }
         }
+        team_sync<WAVE>();                                  // res has been read
     }
     if (parts == nullptr) return;
     // the rows of a team, or where every team has the one slab of all the workgroup's, together, channel by channel
-    const int width = l.hi - l.lo;
     const bool together = !WAVE || q.slabs == 1;
     const int teams_here = WAVE && together ? TH / q.ts : 1, size = teams_here * q.ts * V, slot = (WAVE && together ? tid / q.ts * q.slots : 0) + l.slot;
-    float* const sums = WAVE && together ? red : myred;
+    float* const sums = WAVE && together ? red : red + 2 * base * V;
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v)
         if (l.own[v]) {
-            sums[slot * width + l.c + v - l.lo] = accb[v];
-            sums[size + slot * width + l.c + v - l.lo] = accg[v];
+            sums[slot * l.width + l.c + v - l.lo] = accb[v];
+            sums[size + slot * l.width + l.c + v - l.lo] = accg[v];
         }
     __syncthreads();
     if (team >= teams && !together) return;
-    float2* const to = parts + (size_t)(together ? (WAVE ? (int)blockIdx.x : team / q.slabs) : team / q.slabs) * p.C + l.lo;
-    for (int c = WAVE && together ? tid : lt; c < width; c += WAVE && together ? TH : q.ts) {
+    float2* const to = parts + (size_t)(WAVE && together ? (int)blockIdx.x : team / q.slabs) * p.C + l.lo;
+    for (int c = WAVE && together ? tid : lt; c < l.width; c += WAVE && together ? TH : q.ts) {
         float b = 0.0f, g = 0.0f;
-        for (int s = 0; s < teams_here * q.slots; ++s) { b += sums[s * width + c]; g += sums[size + s * width + c]; }
+        for (int s = 0; s < teams_here * q.slots; ++s) { b += sums[s * l.width + c]; g += sums[size + s * l.width + c]; }
         to[c] = make_float2(b, g);
     }
 }
 
-// dbeta and dgamma from E parts of them: 64 channels x 16 shares of the parts per workgroup, joined in order.
-__global__ __launch_bounds__(1024) void group_norm_params_kernel(const float2* parts, int E, int C, float* dgamma, float* dbeta) {
-    __shared__ float2 red[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+// dbeta and dgamma from E parts of them: 16 channels x 64 shares of the parts per workgroup, joined in order.
+__device__ __forceinline__ void join_params(const float2* parts, int E, int C, float* dgamma, float* dbeta, int block, int share, int shares, int lane,
+                                            float2 (*red)[16]) {
+    const int c = block * 16 + lane;
     float2 s = make_float2(0.0f, 0.0f);
     if (c < C)
-        for (int k = w; k < E; k += 16) {
+        for (int k = share; k < E; k += shares) {
             const float2 t = parts[(size_t)k * C + c];
             s.x += t.x; s.y += t.y;
         }
-    red[w][lane] = s;
+    red[share][lane] = s;
     __syncthreads();
-    if (w == 0 && c < C) {
-        for (int k = 1; k < 16; ++k) { s.x += red[k][lane].x; s.y += red[k][lane].y; }
+    if (share == 0 && c < C) {
+        for (int k = 1; k < shares; ++k) { s.x += red[k][lane].x; s.y += red[k][lane].y; }
         if (dbeta) dbeta[c] = s.x;
         if (dgamma) dgamma[c] = s.y;
     }
 }
-
-// ---- split form.  A workgroup has a tile: slots x K rows of an item's slab.
-constexpr int kTileThreads = 256;
-struct Tile { long long n; int chunk, slab; };
-__device__ __forceinline__ Tile tile_of(const Geo& q, int chunks) {
-    Tile t;
-    t.slab = blockIdx.x % q.slabs;
-    const unsigned r = blockIdx.x / q.slabs;
-    t.chunk = r % chunks;
-    t.n = r / chunks;
-    return t;
+__global__ __launch_bounds__(1024) void group_norm_params_kernel(const float2* parts, int E, int C, float* dgamma, float* dbeta) {
+    __shared__ float2 red[64][16];
+    join_params(parts, E, C, dgamma, dbeta, blockIdx.x, threadIdx.x >> 4, 64, threadIdx.x & 15, red);
 }
 
-// part[(n G + g) E + e] = (rows, mean, squared deviations), E = chunks x spg tiles of a group
-template <typename T, int V, int K>
-__global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const GroupNormArgs p, const Geo q, int chunks, float4* part) {
-    __shared__ float red[kTileThreads * V], mean_of[kTileThreads * V];
-    __shared__ int cnt;
-    const Tile t = tile_of(q, chunks);
-    const Lane<V> l(q, p.C, p.G, t.slab, threadIdx.x);
-    const int r0 = t.chunk * q.slots * K;
-    const long long row0 = t.n * p.P;
-    Pack<T, V> x[K];
-    bool live[K];
-    int mine = 0;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = r0 + l.slot + k * q.slots;
-        const long long row = row0 + min(r, p.P - 1);
-        x[k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
-        live[k] = l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
-        mine += live[k];
+// ---- split form
+constexpr int kTileThreads = 256, kRows = 8;
+struct Tile {
+    long long n;
+    int chunk, slab, r0, r1;             // the tile's positions
+    __device__ Tile(const Geo& q, int chunks, int per, int P) {
+        slab = blockIdx.x % q.slabs;
+        const unsigned r = blockIdx.x / q.slabs;
+        chunk = r % chunks;
+        n = r / chunks;
+        r0 = chunk * per;
+        r1 = min(r0 + per, P);
     }
-    const int rows = p.mask != nullptr ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : min(q.slots * K, p.P - r0);
+};
+// kRows rows of a lane from r on: what they hold, and which of them count
+template <typename T, int V, bool ONE>
+__device__ __forceinline__ void load_rows(const void* x, long long sx, const uint8_t* mask, const Geo& q, const Lane<V, ONE>& l, const Tile& t, long long row0, int r,
+                                          Pack<T, V>* to, bool* live) {
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        const int at = r + l.slot + k * q.slots;
+        const long long row = row0 + min(at, t.r1 - 1);
+        to[k] = load_pack<T, V>(static_cast<const T*>(x) + row * sx + l.c);
+        if (live) live[k] = l.on && at < t.r1 && (mask == nullptr || mask[row] == 0);
+    }
+}
+
+// part[(n G + g) E + e] = (values, mean, squared deviations), E = chunks x spg tiles of a group
+template <typename T, int V, bool ONE>
+__global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float4* part) {
+    constexpr int PER = ONE ? 1 : V;
+    __shared__ float red[kTileThreads * PER], mean_of[kTileThreads * Lane<V, ONE>::GV];
+    __shared__ int cnt;
+    const Tile t(q, chunks, per, p.P);
+    const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
+    const long long row0 = t.n * p.P;
+    float mean[V], m2[V], n = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) mean[v] = m2[v] = 0.0f;
+    int mine = 0;
+    for (int r = t.r0; r < t.r1; r += q.slots * kRows) {
+        Pack<T, V> x[kRows];
+        bool live[kRows];
+        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+        int here = 0;
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) here += live[k];
+        mine += here;
+        const float m = (float)here, inv = here > 0 ? 1.0f / m : 0.0f, share = here > 0 ? m / (n + m) : 0.0f, both = n * share;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float sum = 0.0f, sq = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) sum += live[k] ? get<T, V>(x[k], v) : 0.0f;
+            sum *= inv;                                     // the mean of these rows
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) {
+                const float d = live[k] ? get<T, V>(x[k], v) - sum : 0.0f;
+                sq = fmaf(d, d, sq);
+            }
+            const float d = sum - mean[v];
+            mean[v] = here > 0 ? fmaf(d, share, mean[v]) : mean[v];
+            m2[v] += here > 0 ? fmaf(d * d, both, sq) : 0.0f;
+        }
+        n += m;
+    }
+    const int rows = p.mask != nullptr ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
     const float M = (float)rows * (float)l.D, inv = rows > 0 ? 1.0f / M : 0.0f;
     float s[1][V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        s[0][v] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) s[0][v] += live[k] ? get<T, V>(x[k], v) : 0.0f;
-    }
-    group_sums<V, 1, false>(q, l, red, s, [&](int g, const float* u) { mean_of[g] = u[0] * inv; });
+    for (int v = 0; v < V; ++v) s[0][v] = n * mean[v];
+    group_sums<V, ONE, 1, false>(q, l, red, kTileThreads * PER, s, [&](int g, const float* u) { mean_of[g] = u[0] * inv; });
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const float mean = mean_of[l.group_of(v)];
-        s[0][v] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const float d = live[k] ? get<T, V>(x[k], v) - mean : 0.0f;
-            s[0][v] = fmaf(d, d, s[0][v]);
-        }
+        const float d = n > 0.0f ? mean[v] - mean_of[l.gr[ONE ? 0 : v]] : 0.0f;
+        s[0][v] = fmaf(d * d, n, m2[v]);
     }
     const int E = chunks * q.spg;
-    group_sums<V, 1, false>(q, l, red, s, [&](int g, const float* u) {
+    group_sums<V, ONE, 1, false>(q, l, red, kTileThreads * PER, s, [&](int g, const float* u) {
         part[((size_t)t.n * p.G + l.g0 + g) * E + (size_t)t.chunk * q.spg + t.slab % q.spg] = make_float4(M, mean_of[g], u[0], 0.0f);
     });
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
-    return v;
-}
-// One wavefront per item and group joins its tiles.
-__global__ __launch_bounds__(256) void group_norm_join_kernel(const float4* part, long long groups, int E, float eps, float* stats) {
-    const long long i = blockIdx.x * 4LL + (threadIdx.x >> 6);
-    if (i >= groups) return;
-    const int lane = threadIdx.x & 63;
-    const float4* mine = part + (size_t)i * E;
+// The mean and rstd of a group from its E tiles, by `lanes` lanes (a power of two up to 64, neighbours) of which this is lane `l`.
+__device__ __forceinline__ float2 join_tiles(const float4* tiles, int E, float eps, int l, int lanes) {
     float M = 0.0f, s = 0.0f, m2 = 0.0f;
-    for (int e = lane; e < E; e += 64) { M += mine[e].x; s = fmaf(mine[e].x, mine[e].y, s); }
-    M = wave_sum(M);
-    const float mean = M > 0.0f ? wave_sum(s) / M : 0.0f;
-    for (int e = lane; e < E; e += 64) {
-        const float4 t = mine[e];
+    for (int e = l; e < E; e += lanes) { const float4 t = tiles[e]; M += t.x; s = fmaf(t.x, t.y, s); }
+    for (int m = 1; m < lanes; m <<= 1) { M += __shfl_xor(M, m); s += __shfl_xor(s, m); }
+    const float mean = M > 0.0f ? s / M : 0.0f;
+    for (int e = l; e < E; e += lanes) {
+        const float4 t = tiles[e];
         const float d = t.y - mean;
         m2 += fmaf(t.x * d, d, t.z);
     }
-    m2 = wave_sum(m2);
-    if (lane == 0) {
-        stats[2 * i] = mean;
-        stats[2 * i + 1] = M > 0.0f ? 1.0f / sqrtf(m2 / M + eps) : 0.0f;
+    for (int m = 1; m < lanes; m <<= 1) m2 += __shfl_xor(m2, m);
+    return make_float2(mean, M > 0.0f ? 1.0f / sqrtf(m2 / M + eps) : 0.0f);
+}
+// One wavefront per item and group, where there are too many tiles for every workgroup of the apply kernel to join them by itself.
+__global__ __launch_bounds__(64) void group_norm_join_kernel(const float4* part, int E, float eps, float* stats) {
+    const float2 r = join_tiles(part + (size_t)blockIdx.x * E, E, eps, threadIdx.x, 64);
+    if (threadIdx.x == 0) { stats[2 * (size_t)blockIdx.x] = r.x; stats[2 * (size_t)blockIdx.x + 1] = r.y; }
+}
+
+// part: the tiles, to be joined here, or null: the statistics are there.
+template <typename T, int V, bool ONE, int ACT>
+__global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, const float4* part) {
+    constexpr int GV = Lane<V, ONE>::GV;
+    __shared__ float2 joined[kTileThreads * GV];
+    const Tile t(q, chunks, per, p.P);
+    const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
+    const long long row0 = t.n * p.P;
+    const int batch = q.slots * kRows;
+    float gamma[V], beta[V], mean[GV], rstd[GV];
+    load_params<V>(p, l.c, gamma, beta);
+    if (part != nullptr) {
+        const int E = chunks * q.spg;
+        for (int g = l.lt / q.tpg; g < l.groups; g += kTileThreads / q.tpg) {
+            const size_t at = (size_t)t.n * p.G + l.g0 + g;
+            const float2 r = join_tiles(part + at * E, E, p.eps, l.lt & (q.tpg - 1), q.tpg);
+            if ((l.lt & (q.tpg - 1)) == 0) {
+                joined[g] = r;
+                if (t.chunk == 0 && t.slab % q.spg == 0) { p.stats[2 * at] = r.x; p.stats[2 * at + 1] = r.y; }
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int v = 0; v < GV; ++v) {
+        const float* st = p.stats + ((size_t)t.n * p.G + l.g0 + l.gr[v]) * 2;
+        mean[v] = part != nullptr ? joined[l.gr[v]].x : st[0];
+        rstd[v] = part != nullptr ? joined[l.gr[v]].y : st[1];
+    }
+    if (!l.on) return;
+    for (int r = t.r0 + (t.r1 - 1 - t.r0) / batch * batch; r >= t.r0; r -= batch) {
+        Pack<T, V> x[kRows];
+        bool live[kRows];
+        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int at = r + l.slot + k * q.slots;
+            if (at < t.r1) {
+                float y[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    y[v] = live[k] ? act_of<ACT>(fmaf((get<T, V>(x[k], v) - mean[ONE ? 0 : v]) * rstd[ONE ? 0 : v], gamma[v], beta[v])) : 0.0f;
+                store_own<T, V>(static_cast<T*>(p.y) + (row0 + at) * p.sy + l.c, l, y);
+            }
+        }
     }
 }
 
-template <typename T, int V, int K, int ACT>
-__global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const GroupNormArgs p, const Geo q, int chunks) {
-    const Tile t = tile_of(q, chunks);
-    const Lane<V> l(q, p.C, p.G, t.slab, threadIdx.x);
-    if (!l.on) return;
-    const int r0 = t.chunk * q.slots * K;
+// sums[n][chunk][C] = (sum dv, sum dv xh) of a tile; counts[n][chunk]: its rows that count
+template <typename T, int V, bool ONE, int ACT>
+__global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float2* sums, float* counts) {
+    constexpr int GV = Lane<V, ONE>::GV;
+    __shared__ float red[2][kTileThreads * V];
+    __shared__ int cnt;
+    const Tile t(q, chunks, per, p.P);
+    const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
-    Pack<T, V> x[K];
-    bool live[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = r0 + l.slot + k * q.slots;
-        const long long row = row0 + min(r, p.P - 1);
-        x[k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
-        live[k] = p.mask == nullptr || p.mask[row] == 0;
-    }
-    float gamma[V], beta[V], mean[V], rstd[V];
+    float gamma[V], beta[V], mean[GV], rstd[GV], b[V], g[V];
     load_params<V>(p, l.c, gamma, beta);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const float* st = p.stats + ((size_t)t.n * p.G + l.g0 + l.group_of(v)) * 2;
+    for (int v = 0; v < GV; ++v) {
+        const float* st = p.stats + ((size_t)t.n * p.G + l.g0 + l.gr[v]) * 2;
         mean[v] = st[0];
         rstd[v] = st[1];
     }
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = r0 + l.slot + k * q.slots;
-        if (r < p.P) {
-            float y[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) y[v] = live[k] ? act_of<ACT>(fmaf((get<T, V>(x[k], v) - mean[v]) * rstd[v], gamma[v], beta[v])) : 0.0f;
-            store_own<T, V>(static_cast<T*>(p.y) + (row0 + r) * p.sy + l.c, l, y);
-        }
-    }
-}
-
-// sums[n][chunk][C] = (sum dv, sum dv xh) of a tile; rows[n][chunk]: its rows that count
-template <typename T, int V, int K, int ACT>
-__global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const GroupNormArgs p, const Geo q, int chunks, float2* sums, float* counts) {
-    __shared__ float red[2][kTileThreads * V];
-    __shared__ int cnt;
-    const Tile t = tile_of(q, chunks);
-    const Lane<V> l(q, p.C, p.G, t.slab, threadIdx.x);
-    const int r0 = t.chunk * q.slots * K;
-    const long long row0 = t.n * p.P;
-    Pack<T, V> x[K], dy[K];
-    bool live[K];
+    for (int v = 0; v < V; ++v) b[v] = g[v] = 0.0f;
     int mine = 0;
+    for (int r = t.r0; r < t.r1; r += q.slots * kRows) {
+        Pack<T, V> x[kRows], dy[kRows];
+        bool live[kRows];
+        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+        load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = r0 + l.slot + k * q.slots;
-        const long long row = row0 + min(r, p.P - 1);
-        x[k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
-        dy[k] = load_pack<T, V>(static_cast<const T*>(p.dy) + row * p.sdy + l.c);
-        live[k] = l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
-        mine += live[k];
-    }
-    float gamma[V], beta[V];
-    load_params<V>(p, l.c, gamma, beta);
-    const int width = l.hi - l.lo;
+        for (int k = 0; k < kRows; ++k) {
+            mine += live[k];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const float* st = p.stats + ((size_t)t.n * p.G + l.g0 + l.group_of(v)) * 2;
-        const float mean = st[0], rstd = st[1];
-        float b = 0.0f, g = 0.0f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const float xh = (get<T, V>(x[k], v) - mean) * rstd;
-            const float dv = get<T, V>(dy[k], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v]));
-            b += live[k] ? dv : 0.0f;
-            g += live[k] ? dv * xh : 0.0f;
+            for (int v = 0; v < V; ++v) {
+                const float xh = (get<T, V>(x[k], v) - mean[ONE ? 0 : v]) * rstd[ONE ? 0 : v];
+                const float dv = get<T, V>(dy[k], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v]));
+                b[v] += live[k] ? dv : 0.0f;
+                g[v] += live[k] ? dv * xh : 0.0f;
+            }
         }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
         if (l.own[v]) {
-            red[0][l.slot * width + l.c + v - l.lo] = b;
-            red[1][l.slot * width + l.c + v - l.lo] = g;
+            red[0][l.slot * l.width + l.c + v - l.lo] = b[v];
+            red[1][l.slot * l.width + l.c + v - l.lo] = g[v];
         }
-    }
-    const int rows = p.mask != nullptr ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : min(q.slots * K, p.P - r0);
+    const int rows = p.mask != nullptr ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
     __syncthreads();
-    for (int c = l.lt; c < width; c += kTileThreads) {
-        float b = 0.0f, g = 0.0f;
-        for (int s = 0; s < q.slots; ++s) { b += red[0][s * width + c]; g += red[1][s * width + c]; }
-        sums[((size_t)t.n * chunks + t.chunk) * p.C + l.lo + c] = make_float2(b, g);
+    for (int c = l.lt; c < l.width; c += kTileThreads) {
+        float sb = 0.0f, sg = 0.0f;
+        for (int s = 0; s < q.slots; ++s) { sb += red[0][s * l.width + c]; sg += red[1][s * l.width + c]; }
+        sums[((size_t)t.n * chunks + t.chunk) * p.C + l.lo + c] = make_float2(sb, sg);
     }
     if (t.slab == 0 && threadIdx.x == 0) counts[(size_t)t.n * chunks + t.chunk] = (float)rows;
 }
 
-// 64 channels of an item per workgroup: the tiles' sums joined in order, chan[n][C].
-__global__ __launch_bounds__(1024) void group_norm_chan_kernel(const float2* sums, int chunks, int C, float2* chan) {
-    __shared__ float2 red[16][64];
-    const int cols = (C + 63) / 64, lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = (blockIdx.x % cols) * 64 + lane;
-    const size_t n = blockIdx.x / cols;
-    float2 s = make_float2(0.0f, 0.0f);
-    if (c < C)
-        for (int k = w; k < chunks; k += 16) {
-            const float2 t = sums[(n * chunks + k) * C + c];
-            s.x += t.x; s.y += t.y;
+// Joins the tiles' sums of an item, for some of its groups per workgroup (at least 16 channels, 128 bytes a row): chan[n][C], and
+// coef[n][G] = (sum dv gamma, sum dv gamma xh) / M.  Where there is only one item, its sums are dbeta and dgamma.
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void group_norm_chan_kernel(const float2* sums, const float* counts, int chunks, int C, int G, int D, int gw,
+                                                                       const float* gamma, float2* chan, float2* coef, float* dgamma, float* dbeta) {
+    __shared__ float2 red[kJoinThreads], total[kJoinThreads];
+    __shared__ float rows_of[kJoinThreads / 64];
+    const int tid = threadIdx.x, sets = (G + gw - 1) / gw, g0 = (blockIdx.x % sets) * gw;
+    const size_t n = blockIdx.x / sets;
+    const int groups = min(gw, G - g0), width = groups * D, lo = g0 * D;
+    float rows = 0.0f;
+    for (int k = tid; k < chunks; k += kJoinThreads) rows += counts[n * chunks + k];
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) rows += __shfl_xor(rows, m);
+    if ((tid & 63) == 0) rows_of[tid >> 6] = rows;
+    float2 mine = make_float2(0.0f, 0.0f);                  // of a group's gamma-weighted sums, in the lanes that keep them
+    for (int c0 = 0; c0 < width; c0 += kJoinThreads) {      // more than one turn only for a group of more channels than threads
+        const int w = min(width - c0, kJoinThreads), shares = kJoinThreads / w, c = tid % w, share = tid / w;
+        float2 s = make_float2(0.0f, 0.0f);
+        if (share < shares)
+            for (int k = share; k < chunks; k += shares) {
+                const float2 t = sums[(n * chunks + k) * C + lo + c0 + c];
+                s.x += t.x; s.y += t.y;
+            }
+        __syncthreads();
+        red[tid] = s;
+        __syncthreads();
+        if (tid < w) {
+            for (int k = 1; k < shares; ++k) { s.x += red[k * w + c].x; s.y += red[k * w + c].y; }
+            const int ch = lo + c0 + c;
+            if (chan) chan[n * C + ch] = s;
+            if (dbeta) dbeta[ch] = s.x;
+            if (dgamma) dgamma[ch] = s.y;
+            const float gm = gamma ? gamma[ch] : 1.0f;
+            total[tid] = make_float2(s.x * gm, s.y * gm);
         }
-    red[w][lane] = s;
-    __syncthreads();
-    if (w == 0 && c < C) {
-        for (int k = 1; k < 16; ++k) { s.x += red[k][lane].x; s.y += red[k][lane].y; }
-        chan[n * C + c] = s;
+        __syncthreads();
+        if (groups == 1) {                                  // all threads on one group
+            if (tid < w) { mine.x += total[tid].x; mine.y += total[tid].y; }
+        } else if (tid < groups) {
+            for (int d = 0; d < D; ++d) { mine.x += total[tid * D + d].x; mine.y += total[tid * D + d].y; }
+        }
     }
-}
-// One wavefront per item and group: coef[n][G] = (sum dv gamma, sum dv gamma xh) / M.
-__global__ __launch_bounds__(256) void group_norm_coef_kernel(const float2* chan, const float* counts, int chunks, const float* gamma, long long groups,
-                                                              int G, int D, float2* coef) {
-    const long long i = blockIdx.x * 4LL + (threadIdx.x >> 6);
-    if (i >= groups) return;
-    const int lane = threadIdx.x & 63, g = (int)(i % G);
-    const long long n = i / G;
-    float rows = 0.0f, a = 0.0f, b = 0.0f;
-    for (int k = lane; k < chunks; k += 64) rows += counts[n * chunks + k];
-    for (int d = lane; d < D; d += 64) {
-        const float2 t = chan[((size_t)n * G + g) * D + d];
-        const float gm = gamma ? gamma[g * D + d] : 1.0f;
-        a = fmaf(t.x, gm, a);
-        b = fmaf(t.y, gm, b);
+    if (groups == 1) {
+        __syncthreads();
+        total[tid] = mine;
+        for (int m = kJoinThreads / 2; m > 0; m >>= 1) {
+            __syncthreads();
+            if (tid < m) { total[tid].x += total[tid + m].x; total[tid].y += total[tid + m].y; }
+        }
+        mine = total[0];
     }
-    rows = wave_sum(rows); a = wave_sum(a); b = wave_sum(b);
-    const float inv = rows > 0.0f ? 1.0f / (rows * (float)D) : 0.0f;
-    if (lane == 0) coef[i] = make_float2(a * inv, b * inv);
+    if (tid < groups) {
+        float M = 0.0f;
+        for (int k = 0; k < kJoinThreads / 64; ++k) M += rows_of[k];
+        const float inv = M > 0.0f ? 1.0f / (M * (float)D) : 0.0f;
+        coef[n * G + g0 + tid] = make_float2(mine.x * inv, mine.y * inv);
+    }
 }
 
-template <typename T, int V, int K, int ACT>
-__global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const GroupNormArgs p, const Geo q, int chunks, const float2* coef) {
-    const Tile t = tile_of(q, chunks);
-    const Lane<V> l(q, p.C, p.G, t.slab, threadIdx.x);
-    if (!l.on) return;
-    const int r0 = t.chunk * q.slots * K;
-    const long long row0 = t.n * p.P;
-    Pack<T, V> x[K], dy[K];
-    bool live[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = r0 + l.slot + k * q.slots;
-        const long long row = row0 + min(r, p.P - 1);
-        x[k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
-        dy[k] = load_pack<T, V>(static_cast<const T*>(p.dy) + row * p.sdy + l.c);
-        live[k] = p.mask == nullptr || p.mask[row] == 0;
+// The workgroups behind the tiles' join the items' sums to dbeta and dgamma.
+template <typename T, int V, bool ONE, int ACT>
+__global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, const float2* coef, unsigned tiles,
+                                                                       const float2* chan) {
+    constexpr int GV = Lane<V, ONE>::GV;
+    __shared__ float2 red[kTileThreads / 16][16];
+    if (blockIdx.x >= tiles) {
+        join_params(chan, p.N, p.C, p.dgamma, p.dbeta, blockIdx.x - tiles, threadIdx.x >> 4, kTileThreads / 16, threadIdx.x & 15, red);
+        return;
     }
-    float gamma[V], beta[V], mean[V], rstd[V], s1[V], s2[V];
+    const Tile t(q, chunks, per, p.P);
+    const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
+    if (!l.on) return;
+    const long long row0 = t.n * p.P;
+    const int batch = q.slots * kRows;
+    float gamma[V], beta[V], mean[GV], rstd[GV], s1[GV], s2[GV];
     load_params<V>(p, l.c, gamma, beta);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const size_t at = (size_t)t.n * p.G + l.g0 + l.group_of(v);
+    for (int v = 0; v < GV; ++v) {
+        const size_t at = (size_t)t.n * p.G + l.g0 + l.gr[v];
         mean[v] = p.stats[2 * at];
         rstd[v] = p.stats[2 * at + 1];
         s1[v] = coef[at].x;
         s2[v] = coef[at].y;
     }
+    for (int r = t.r0 + (t.r1 - 1 - t.r0) / batch * batch; r >= t.r0; r -= batch) {
+        Pack<T, V> x[kRows], dy[kRows];
+        bool live[kRows];
+        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+        load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = r0 + l.slot + k * q.slots;
-        if (r < p.P) {
-            float dx[V];
+        for (int k = 0; k < kRows; ++k) {
+            const int at = r + l.slot + k * q.slots;
+            if (at < t.r1) {
+                float dx[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float xh = (get<T, V>(x[k], v) - mean[v]) * rstd[v];
-                const float dv = get<T, V>(dy[k], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v]));
-                dx[v] = live[k] ? rstd[v] * (fmaf(dv, gamma[v], -s1[v]) - xh * s2[v]) : 0.0f;
+                for (int v = 0; v < V; ++v) {
+                    const int w = ONE ? 0 : v;
+                    const float xh = (get<T, V>(x[k], v) - mean[w]) * rstd[w];
+                    const float dv = get<T, V>(dy[k], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v]));
+                    dx[v] = live[k] ? rstd[w] * (fmaf(dv, gamma[v], -s1[w]) - xh * s2[w]) : 0.0f;
+                }
+                store_own<T, V>(static_cast<T*>(p.dx) + (row0 + at) * p.sdx + l.c, l, dx);
             }
-            store_own<T, V>(static_cast<T*>(p.dx) + (row0 + r) * p.sdx + l.c, l, dx);
         }
     }
 }
 
 // ---- shapes
 constexpr int kMaxWgs = 2048;            // workgroups of the held form: eight per compute unit
+constexpr int kTileWgs = 1024;           // tiles of the split form, at least, where there are rows enough: four per compute unit
 enum { FORM_WAVE = 0, FORM_GROUP = 1, FORM_SPLIT = 2 };
-constexpr int kHeldRows = 8, kWaveThreads = 256, kGroupThreads = 512, kTileRows = 8;
+constexpr int kHeldRows = 8, kWaveThreads = 256, kGroupThreads = 512;
+constexpr int kItems = 4, kItemsBwd = 2;                   // single rows that a lane takes at once
 
 int floor_pow2(int v) {
     int r = 1;
@@ -647,9 +773,10 @@ int floor_pow2(int v) {
 }
 struct NormPlan {
     int form, V, K;                      // K: rows of a lane
+    bool one;                            // V divides the channels of a group
     Geo q;
     long long teams, parts;              // held forms; parts of the parameters' sums
-    int chunks;                          // split form
+    int chunks, per;                     // split form: tiles of an item, positions of a tile
 };
 // Slabs of at most `most` channels for teams of ts lanes; false where a group is wider than that and has to be whole.
 bool fill_geo(const scan2d_group_norm_desc* d, int V, int ts, int most, bool whole, Geo* q) {
@@ -665,7 +792,7 @@ bool fill_geo(const scan2d_group_norm_desc* d, int V, int ts, int most, bool who
     } else {
         if (whole) return false;
         q->spg = (D + most - 1) / most;
-        q->width = (D + q->spg - 1) / q->spg;
+        q->width = ((D + q->spg - 1) / q->spg + V - 1) / V * V;
         q->spg = (D + q->width - 1) / q->width;
         q->gps = 1;
         q->slabs = d->G * q->spg;
@@ -682,6 +809,7 @@ NormPlan plan_of(const scan2d_group_norm_desc* d) {
     NormPlan n = {};
     n.V = d->C >= 4 ? 4 : 1;
     const int D = d->C / d->G;
+    n.one = D % n.V == 0;
     const auto held = [&](int form, long long most_teams) {
         n.form = form;
         n.K = n.q.slots >= d->P && n.V > 1 ? 1 : kHeldRows;
@@ -706,50 +834,68 @@ NormPlan plan_of(const scan2d_group_norm_desc* d) {
     }
     n.form = FORM_SPLIT;
     (void)fill_geo(d, n.V, kTileThreads, kTileThreads * n.V, false, &n.q);
-    n.chunks = (int)((d->P + (long long)n.q.slots * kTileRows - 1) / ((long long)n.q.slots * kTileRows));
+    const long long batch = (long long)n.q.slots * kRows, batches = (d->P + batch - 1) / batch, each = (long long)d->N * n.q.slabs;
+    long long chunks = (kTileWgs + each - 1) / each;
+    if (chunks > batches) chunks = batches;
+    const long long per = (batches + chunks - 1) / chunks * batch;
+    n.per = (int)(per < d->P ? per : d->P);
+    n.chunks = (int)((d->P + n.per - 1) / n.per);
     return n;
 }
+// Whether every workgroup of the apply kernel joins the tiles of its groups by itself: up to 2048 of them, eight to a lane, while
+// a kernel of its own costs about 4 us.
+bool join_in_apply(const NormPlan& n) { return (long long)n.chunks * n.q.spg * n.q.gps <= 2048; }
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 int launched() { return hipGetLastError() == hipSuccess ? SCAN2D_OK : SCAN2D_ERR_LAUNCH_FAILED; }
 
-template <typename T, int V, int ACT>
+template <typename T, int V, bool ONE, int ACT>
 int fwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     if (n.form != FORM_SPLIT) {
         using Kernel = void (*)(const GroupNormArgs, const Geo, int);
         const bool wave = n.form == FORM_WAVE;
-        Kernel k = wave ? group_norm_fwd_kernel<T, V, kHeldRows, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, kHeldRows, kGroupThreads, false, ACT>;
+        Kernel k = wave ? group_norm_fwd_kernel<T, V, ONE, kHeldRows, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, kHeldRows, 1, kGroupThreads, false, ACT>;
         if constexpr (V > 1)
-            if (n.K == 1) k = wave ? group_norm_fwd_kernel<T, V, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, 1, kGroupThreads, false, ACT>;
+            if (n.K == 1) {
+                // one item per team: none that it could take besides
+                if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
+                else k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, kItems, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, kItems, kGroupThreads, false, ACT>;
+            }
         const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
         hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams);
         return launched();
     }
     const long long blocks = (long long)a.N * n.chunks * n.q.slabs, groups = (long long)a.N * a.G;
-    if (!launch_fits(blocks, kTileThreads) || !launch_fits(groups / 4 + 1, 256)) return SCAN2D_ERR_BAD_SHAPE;
+    if (!launch_fits(blocks, kTileThreads) || !launch_fits(groups, 64)) return SCAN2D_ERR_BAD_SHAPE;
     float4* part = static_cast<float4*>(a.workspace);
-    hipLaunchKernelGGL((group_norm_tiles_kernel<T, V, kTileRows>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, part);
-    hipLaunchKernelGGL(group_norm_join_kernel, dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, stream, part, groups, n.chunks * n.q.spg, a.eps, a.stats);
-    hipLaunchKernelGGL((group_norm_apply_kernel<T, V, kTileRows, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks);
+    const bool in_apply = join_in_apply(n);
+    hipLaunchKernelGGL((group_norm_tiles_kernel<T, V, ONE>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, part);
+    if (!in_apply)
+        hipLaunchKernelGGL(group_norm_join_kernel, dim3((unsigned)groups), dim3(64), 0, stream, part, n.chunks * n.q.spg, a.eps, a.stats);
+    hipLaunchKernelGGL((group_norm_apply_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, in_apply ? part : nullptr);
     return launched();
 }
-template <typename T, int V, int ACT>
+template <typename T, int V, bool ONE, int ACT>
 int bwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
-    const dim3 cols((a.C + 63) / 64);
+    const unsigned cols = (a.C + 15) / 16;
     if (n.form != FORM_SPLIT) {
         using Kernel = void (*)(const GroupNormArgs, const Geo, int, float2*);
         const bool wave = n.form == FORM_WAVE;
         float2* parts = params ? static_cast<float2*>(a.workspace) : nullptr;
-        Kernel k = wave ? group_norm_bwd_kernel<T, V, kHeldRows, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, kHeldRows, kGroupThreads, false, ACT>;
+        Kernel k = wave ? group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kGroupThreads, false, ACT>;
         if constexpr (V > 1)
-            if (n.K == 1) k = wave ? group_norm_bwd_kernel<T, V, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, 1, kGroupThreads, false, ACT>;
+            if (n.K == 1) {
+                if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
+                else k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kGroupThreads, false, ACT>;
+            }
         const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
         hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams, parts);
-        if (params) hipLaunchKernelGGL(group_norm_params_kernel, cols, dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
+        if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3(cols), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
         return launched();
     }
-    const long long blocks = (long long)a.N * n.chunks * n.q.slabs, groups = (long long)a.N * a.G;
-    if (!launch_fits(blocks, kTileThreads) || !launch_fits(groups / 4 + 1, 256) || !launch_fits((long long)a.N * cols.x, 1024)) return SCAN2D_ERR_BAD_SHAPE;
+    const int gw = a.D >= 16 ? 1 : (16 + a.D - 1) / a.D, sets = (a.G + gw - 1) / gw;
+    const long long blocks = (long long)a.N * n.chunks * n.q.slabs, joins = (long long)a.N * sets;
+    if (!launch_fits(blocks + cols, kTileThreads) || !launch_fits(joins, kJoinThreads)) return SCAN2D_ERR_BAD_SHAPE;
     char* w = static_cast<char*>(a.workspace);
     const size_t items = (size_t)a.N * n.chunks;
     float2* sums = reinterpret_cast<float2*>(w);
@@ -759,27 +905,32 @@ int bwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     float2* chan = reinterpret_cast<float2*>(w);
     w += up((size_t)a.N * a.C * sizeof(float2));
     float2* coef = reinterpret_cast<float2*>(w);
-    hipLaunchKernelGGL((group_norm_sums_kernel<T, V, kTileRows, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, sums, counts);
-    hipLaunchKernelGGL(group_norm_chan_kernel, dim3((unsigned)(a.N * cols.x)), dim3(1024), 0, stream, sums, n.chunks, a.C, chan);
-    hipLaunchKernelGGL(group_norm_coef_kernel, dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, stream, chan, counts, n.chunks, a.gamma, groups, a.G, a.D, coef);
-    hipLaunchKernelGGL((group_norm_grad_kernel<T, V, kTileRows, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, coef);
-    if (params) hipLaunchKernelGGL(group_norm_params_kernel, cols, dim3(1024), 0, stream, chan, a.N, a.C, a.dgamma, a.dbeta);
+    const bool several = params && a.N > 1;
+    hipLaunchKernelGGL((group_norm_sums_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, sums, counts);
+    hipLaunchKernelGGL(group_norm_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, a.C, a.G, a.D, gw, a.gamma,
+                       several ? chan : nullptr, coef, several ? nullptr : a.dgamma, several ? nullptr : a.dbeta);
+    hipLaunchKernelGGL((group_norm_grad_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks + (several ? cols : 0)), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, coef,
+                       (unsigned)blocks, chan);
     return launched();
 }
 
-template <typename T, int V>
+template <typename T, int V, bool ONE>
 int by_act(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
     (void)hipGetLastError();
     switch (a.act) {
-        case SCAN2D_ACT_SILU: return backward ? bwd<T, V, SCAN2D_ACT_SILU>(a, n, stream) : fwd<T, V, SCAN2D_ACT_SILU>(a, n, stream);
-        case SCAN2D_ACT_GELU: return backward ? bwd<T, V, SCAN2D_ACT_GELU>(a, n, stream) : fwd<T, V, SCAN2D_ACT_GELU>(a, n, stream);
-        default: return backward ? bwd<T, V, SCAN2D_ACT_NONE>(a, n, stream) : fwd<T, V, SCAN2D_ACT_NONE>(a, n, stream);
+        case SCAN2D_ACT_SILU: return backward ? bwd<T, V, ONE, SCAN2D_ACT_SILU>(a, n, stream) : fwd<T, V, ONE, SCAN2D_ACT_SILU>(a, n, stream);
+        case SCAN2D_ACT_GELU: return backward ? bwd<T, V, ONE, SCAN2D_ACT_GELU>(a, n, stream) : fwd<T, V, ONE, SCAN2D_ACT_GELU>(a, n, stream);
+        default: return backward ? bwd<T, V, ONE, SCAN2D_ACT_NONE>(a, n, stream) : fwd<T, V, ONE, SCAN2D_ACT_NONE>(a, n, stream);
     }
+}
+template <typename T>
+int by_lane(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
+    if (n.V == 1) return by_act<T, 1, true>(a, n, backward, stream);
+    return n.one ? by_act<T, 4, true>(a, n, backward, stream) : by_act<T, 4, false>(a, n, backward, stream);
 }
 int dispatch(const scan2d_group_norm_desc* d, const GroupNormArgs& a, bool backward, hipStream_t stream) {
     const NormPlan n = plan_of(d);
-    if (d->dtype == SCAN2D_BF16) return n.V == 1 ? by_act<bf16_t, 1>(a, n, backward, stream) : by_act<bf16_t, 4>(a, n, backward, stream);
-    return n.V == 1 ? by_act<float, 1>(a, n, backward, stream) : by_act<float, 4>(a, n, backward, stream);
+    return d->dtype == SCAN2D_BF16 ? by_lane<bf16_t>(a, n, backward, stream) : by_lane<float>(a, n, backward, stream);
 }
 
 }  // namespace

@@ -27,7 +27,7 @@
 namespace scan2d {
 namespace {
 
-constexpr int kGroup = 16;               // chunks between the states that the chain hands on
+constexpr int kTeam = 4, kTeams = 8, kGroup = kTeam * kTeams;     // chunks of a team, teams of a group
 constexpr int kSavedRows = 64;           // rows between the states that the forward saves: a chunk of the backward
 
 __device__ __forceinline__ float sigmoid(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t * kLog2e)); }
@@ -59,7 +59,10 @@ __device__ __forceinline__ Pack<T, V> load_pack(uint64_t row, uint32_t offset) {
     Pack<T, V> r;
     if constexpr (V * Elem<T>::kBytes == 2) r.w[0] = *reinterpret_cast<__attribute__((address_space(1))) const u16_a1*>(p);
     else if constexpr (V * Elem<T>::kBytes == 4) r.w[0] = *reinterpret_cast<__attribute__((address_space(1))) const u32_a1*>(p);
-    else {
+    else if constexpr (V * Elem<T>::kBytes == 16) {
+        const u32x4_a1 v = *reinterpret_cast<__attribute__((address_space(1))) const u32x4_a1*>(p);
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+    } else {
         static_assert(V * Elem<T>::kBytes == 8, "two dwords");
         const u32x2_a1 v = *reinterpret_cast<__attribute__((address_space(1))) const u32x2_a1*>(p);
         r.w[0] = v.x; r.w[1] = v.y;
@@ -73,10 +76,15 @@ __device__ __forceinline__ void store_pack(uint64_t row, uint32_t offset, const 
     const gmut p = (gmut)row + offset;
     if constexpr (V == 1 && Elem<T>::kBytes == 2) *reinterpret_cast<__attribute__((address_space(1))) u16_a1*>(p) = (uint16_t)f32_to_bf16_bits(v[0]);
     else if constexpr (V == 1) *reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p) = __float_as_uint(v[0]);
-    else if constexpr (Elem<T>::kBytes == 2) *reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p) = pack_bf16x2(v[0], v[1]);
-    else {
+    else if constexpr (V == 2 && Elem<T>::kBytes == 2) *reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p) = pack_bf16x2(v[0], v[1]);
+    else if constexpr (V * Elem<T>::kBytes == 16) {
+        u32x4_a1 w;
+        w.x = __float_as_uint(v[0]); w.y = __float_as_uint(v[1]); w.z = __float_as_uint(v[2]); w.w = __float_as_uint(v[3]);
+        *reinterpret_cast<__attribute__((address_space(1))) u32x4_a1*>(p) = w;
+    } else {
         u32x2_a1 w;
-        w.x = __float_as_uint(v[0]); w.y = __float_as_uint(v[1]);
+        if constexpr (Elem<T>::kBytes == 2) { w.x = pack_bf16x2(v[0], v[1]); w.y = pack_bf16x2(v[2], v[3]); }
+        else { w.x = __float_as_uint(v[0]); w.y = __float_as_uint(v[1]); }
         *reinterpret_cast<__attribute__((address_space(1))) u32x2_a1*>(p) = w;
     }
 }
@@ -209,8 +217,8 @@ __device__ __forceinline__ void pass_empty(const RecurArgs& p, const float* from
 }
 
 // ---- the chain of chunks
-// Workspace: a counter per column of workgroups (64 bytes each), then per chunk and channel the map (A, S), then per
-// group and channel the state behind it.  All bits set: not written.
+// Workspace: a counter per column of workgroups (64 bytes each), then per chunk the maps (A, S) of its channels (behind the last chunk
+// of a team: of the whole team), then per group the states behind it.  All bits set: not written.
 constexpr uint32_t kUnset = 0xffffffffu;
 __host__ __device__ inline size_t chain_counters(int cols) { return (size_t)cols * 8; }               // in 64-bit words
 __host__ __device__ inline size_t chain_words(int chunks, int cols, int width) {
@@ -223,34 +231,23 @@ __device__ __forceinline__ uint64_t chain_word(float hi, float lo) {
     return ((uint64_t)h << 32) | __float_as_uint(lo);
 }
 __device__ __forceinline__ void chain_put(uint64_t* w, uint64_t v) { __hip_atomic_store(w, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-template <int V>
-__device__ __forceinline__ void chain_get(const uint64_t* w, uint64_t* v) {
-    for (;;) {
-        bool all = true;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            v[k] = __hip_atomic_load(w + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            all = all && (uint32_t)(v[k] >> 32) != kUnset;
-        }
-        if (__all(all)) return;
-        __builtin_amdgcn_s_sleep(1);
-    }
-}
+__device__ __forceinline__ uint64_t chain_get(const uint64_t* w) { return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool is_set(uint64_t w) { return (uint32_t)(w >> 32) != kUnset; }
 
 __global__ __launch_bounds__(256) void recur_clear_kernel(uint4* w, size_t n) {
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (i < n) w[i] = make_uint4(kUnset, kUnset, kUnset, kUnset);
 }
 
-template <int V>
+template <int V, int NW>
 struct ChainLds {
-    float A[kGroup][64 * V], S[kGroup][64 * V];
+    float A[kTeams][64 * V], S[kTeams][64 * V], state[64 * V];
     float decay[64 * V];
     int ticket;
 };
 // The chunk this workgroup is to do, the next of its column's, and its channels' decays.
-template <int V>
-__device__ __forceinline__ int chain_start(const RecurArgs& p, uint64_t* ws, int chunks, int cols, int col, ChainLds<V>& lds) {
+template <int V, int NW>
+__device__ __forceinline__ int chain_start(const RecurArgs& p, uint64_t* ws, int chunks, int cols, int col, ChainLds<V, NW>& lds) {
     constexpr int WIDTH = 64 * V;
     if (chunks > 1 && threadIdx.x == 0) lds.ticket = (int)(atomicAdd(reinterpret_cast<uint32_t*>(ws + (size_t)col * 8), 1u) + 1u);
     const int c = (int)blockDim.x - 1 - (int)threadIdx.x;   // from the last wavefront on: the first waits for its ticket
@@ -258,48 +255,98 @@ __device__ __forceinline__ int chain_start(const RecurArgs& p, uint64_t* ws, int
     __syncthreads();
     return chunks > 1 ? __builtin_amdgcn_readfirstlane(lds.ticket) : 0;
 }
-// The value in front of chunk k (in the order of the scan) for this lane's channels, where the map of chunk k itself is
-// (A, S); every wavefront gets it.  `needed` (the same for the whole workgroup): whether chunk k has use for it.
+// Waits for the words of one chunk or group, V per lane.
+template <int V>
+__device__ __forceinline__ void chain_wait(const uint64_t* w, uint64_t* v) {
+    for (;;) {
+        bool all = true;
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            v[q] = chain_get(w + q * 64);
+            all = all && is_set(v[q]);
+        }
+        if (__all(all)) return;
+        __builtin_amdgcn_s_sleep(1);
+    }
+}
+// The value in front of chunk k (in the order of the scan) for this lane's channels, where the map of chunk k itself is (A, S);
+// every wavefront gets it.  kTeam chunks make a team, kTeams teams a group.  A chunk reads the maps of its team in front of
+// it (the first wavefront, at most 3), those of the group's teams in front of that (one for each further wavefront, at most 7) and
+// the state behind the group before (the last wavefront): 6 reads on average.  These reads pass by the L2 and count: with one level of 32
+// chunks (16 reads, the state by every wavefront) 65536 x 2048 bf16 took 287 us forward, without any 221.
+// The map of a team does not wait for other teams, nor that of a chunk for anything, so only the states, one per group, are a chain.
 template <int V, int NW>
-__device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int col, int k, bool needed, const float* A, const float* S, float* carry,
-                                      ChainLds<V>& lds) {
+__device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int col, int k, const float* A, const float* S, float* carry, ChainLds<V, NW>& lds) {
     constexpr int WIDTH = 64 * V;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = k / kGroup, j = k % kGroup;
-    uint64_t* maps = ws + chain_counters(cols) + (size_t)col * WIDTH + lane * V;
+    static_assert(NW >= kTeams, "a wavefront for each team");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int g = k / kGroup, j = k % kGroup, team = j / kTeam, q = j % kTeam;
+    uint64_t* maps = ws + chain_counters(cols) + (size_t)col * WIDTH + lane;
     uint64_t* states = maps + (size_t)chunks * cols * WIDTH;
     const size_t step = (size_t)cols * WIDTH;
     const bool end = j == kGroup - 1 || k == chunks - 1;    // nobody reads the map of a group's last chunk
-    if (wave == 0 && !end) {
+    if (wave == 0) {
+        if (!end && q != kTeam - 1) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) chain_put(maps + (size_t)k * step + v, chain_word(A[v], S[v]));
-    }
+            for (int v = 0; v < V; ++v) chain_put(maps + (size_t)k * step + v * 64, chain_word(A[v], S[v]));
+        }
+        uint64_t w[kTeam - 1][V];
+        for (bool all = false; !all;) {
+            all = true;
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = 0.0f;
-    const bool hand_on = j == kGroup - 1 && k != chunks - 1;
-    if (needed) {
-        // slot 0: the state behind the group before; slot m: the map of the group's chunk m - 1
-        for (int m = wave; m <= j; m += NW) {
-            if (m == 0 && g == 0) continue;
-            uint64_t w[V];
-            chain_get<V>(m == 0 ? states + (size_t)(g - 1) * step : maps + (size_t)(g * kGroup + m - 1) * step, w);
+            for (int m = 0; m < kTeam - 1; ++m)
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                lds.A[m][lane * V + v] = __uint_as_float((uint32_t)(w[v] >> 32));
-                lds.S[m][lane * V + v] = __uint_as_float((uint32_t)w[v]);
+                for (int v = 0; v < V; ++v) {
+                    w[m][v] = 0x3f80000000000000ull;        // h -> 1 h + 0
+                    if (m < q) {
+                        w[m][v] = chain_get(maps + (size_t)(k - q + m) * step + v * 64);
+                        all = all && is_set(w[m][v]);
+                    }
+                }
+            all = __all(all);
+            if (!all) __builtin_amdgcn_s_sleep(1);
+        }
+        float tA[V], tS[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            tA[v] = 1.0f;
+            tS[v] = 0.0f;
+#pragma unroll
+            for (int m = 0; m < kTeam - 1; ++m) {
+                const float a = __uint_as_float((uint32_t)(w[m][v] >> 32));
+                tS[v] = apply(a, tS[v], __uint_as_float((uint32_t)w[m][v]));
+                tA[v] = compose(tA[v], a);
             }
+            lds.A[0][lane * V + v] = tA[v];
+            lds.S[0][lane * V + v] = tS[v];
+            if (!end && q == kTeam - 1) chain_put(maps + (size_t)k * step + v * 64, chain_word(compose(tA[v], A[v]), apply(A[v], tS[v], S[v])));
         }
-        __syncthreads();
-        if (g > 0) {
+    } else if (wave <= team) {
+        uint64_t w[V];
+        chain_wait<V>(maps + (size_t)(g * kGroup + wave * kTeam - 1) * step, w);
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = lds.S[0][lane * V + v];
+        for (int v = 0; v < V; ++v) {
+            lds.A[wave][lane * V + v] = __uint_as_float((uint32_t)(w[v] >> 32));
+            lds.S[wave][lane * V + v] = __uint_as_float((uint32_t)w[v]);
         }
-        for (int m = 1; m <= j; ++m)
-#pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = apply(lds.A[m][lane * V + v], carry[v], lds.S[m][lane * V + v]);
     }
-    if (wave == 0 && hand_on) {
+    if (wave == NW - 1) {
+        uint64_t w[V];
+        if (g > 0) chain_wait<V>(states + (size_t)(g - 1) * step, w);
 #pragma unroll
-        for (int v = 0; v < V; ++v) chain_put(states + (size_t)g * step + v, chain_word(0.0f, apply(A[v], carry[v], S[v])));
+        for (int v = 0; v < V; ++v) lds.state[lane * V + v] = g > 0 ? __uint_as_float((uint32_t)w[v]) : 0.0f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry[v] = lds.state[lane * V + v];
+    for (int w = 1; w <= team; ++w)
+#pragma unroll
+        for (int v = 0; v < V; ++v) carry[v] = apply(lds.A[w][lane * V + v], carry[v], lds.S[w][lane * V + v]);
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry[v] = apply(lds.A[0][lane * V + v], carry[v], lds.S[0][lane * V + v]);
+    if (wave == 0 && j == kGroup - 1 && k != chunks - 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) chain_put(states + (size_t)g * step + v * 64, chain_word(0.0f, apply(A[v], carry[v], S[v])));
     }
 }
 
@@ -366,11 +413,11 @@ template <typename T, int V, int TW, int NW>
 __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, int chunks, int cols) {
     constexpr int WIDTH = 64 * V, EB = Elem<T>::kBytes;
     __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH];
-    __shared__ ChainLds<V> lds;
+    __shared__ ChainLds<V, NW> lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
     uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
     const SeqSearch search(p);
-    const int k = chain_start<V>(p, ws, chunks, cols, col, lds);
+    const int k = chain_start<V, NW>(p, ws, chunks, cols, col, lds);
     const int c = min(col * WIDTH + lane * V, p.C - V);     // the lanes past the last channels do those again
     const uint32_t off = (uint32_t)c * EB;
     const int t0 = (k * NW + wave) * TW;
@@ -411,7 +458,7 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
                 S[v] = apply(mapA[w][lane * V + v], S[v], mapS[w][lane * V + v]);
                 A[v] = compose(A[v], mapA[w][lane * V + v]);
             }
-        chain<V, NW>(ws, chunks, cols, col, k, k > 0, A, S, h, lds);
+        chain<V, NW>(ws, chunks, cols, col, k, A, S, h, lds);
     }
     for (int w = 0; w < wave; ++w)
 #pragma unroll
@@ -506,11 +553,11 @@ template <typename T, int V, int TW, int NW>
 __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, float* parts, int chunks, int cols) {
     constexpr int WIDTH = 64 * V, EB = Elem<T>::kBytes;
     __shared__ float mapA[NW][WIDTH], mapS[NW][WIDTH], mapD[NW][WIDTH];
-    __shared__ ChainLds<V> lds;
+    __shared__ ChainLds<V, NW> lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = blockIdx.x % cols;
     uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
     const SeqSearch search(p);
-    const int n = chain_start<V>(p, ws, chunks, cols, col, lds), k = chunks - 1 - n;   // the chain runs from the last chunk
+    const int n = chain_start<V, NW>(p, ws, chunks, cols, col, lds), k = chunks - 1 - n;   // the chain runs from the last chunk
     const int c = min(col * WIDTH + lane * V, p.C - V);
     const uint32_t off = (uint32_t)c * EB;
     const int t0 = (k * NW + wave) * TW;
@@ -561,7 +608,7 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
                 D[v] = apply(mapA[w][lane * V + v], D[v], mapD[w][lane * V + v]);
                 A[v] = compose(A[v], mapA[w][lane * V + v]);
             }
-        chain<V, NW>(ws, chunks, cols, col, n, n > 0, A, D, e, lds);
+        chain<V, NW>(ws, chunks, cols, col, n, A, D, e, lds);
     }
     for (int w = NW - 1; w > wave; --w)
 #pragma unroll
@@ -610,32 +657,63 @@ __global__ __launch_bounds__(256) void recur_none_kernel(const float* from, floa
     if (zero && i < C) zero[i] = 0.0f;
 }
 
-// ---- one token per sequence.  One row and 256 channels per workgroup.  A slot that stands at several rows is done by the
-// workgroup of the first of them, in the order of the rows.
-template <typename T>
+// ---- one token per sequence.  One row and 256 V channels per workgroup.  A slot that stands at several rows is done by the
+// workgroup of the first of them, in the order of the rows; all rows' slots are looked through while the row's own loads
+// are under way.
+template <typename T, int V>
 __global__ __launch_bounds__(256) void recur_step_kernel(const RecurArgs p, float* state, const int32_t* slots, long long slot_count) {
-    const int cols = (p.C + 255) / 256, row = blockIdx.x / cols, c = (blockIdx.x % cols) * 256 + threadIdx.x;
+    __shared__ int seen[4];
+    constexpr uint64_t EB = Elem<T>::kBytes;
+    const int cols = (p.C + 256 * V - 1) / (256 * V), row = blockIdx.x / cols, first = ((blockIdx.x % cols) * 256 + threadIdx.x) * V;
+    const int c = min(first, p.C - V), keep = first - c;    // the last lane may have its channels from `keep` on only
     const int slot = slots ? slots[row] : row;
     if (slot < 0 || slot >= slot_count) return;
+    const uint32_t off = (uint32_t)c * (uint32_t)EB;
+    float* const st = state + (size_t)slot * p.C + c;
+    Pack<T, V> x = load_pack<T, V>((uint64_t)p.x + row * p.sx * EB, off), r = load_pack<T, V>((uint64_t)p.r + row * p.sr * EB, off),
+               i = load_pack<T, V>((uint64_t)p.i + row * p.si * EB, off);
+    float h[V], decay[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) { h[v] = st[v]; decay[v] = p.lam[c + v]; }
+    bool again = false;
     if (slots) {
-        int earlier = 0;
-        for (int t = threadIdx.x; t < row; t += 256) earlier |= slots[t] == slot;
-        if (__syncthreads_or(earlier)) return;
+        int found = 0;                                      // 1: at an earlier row, 2: at a later one
+        for (int t = threadIdx.x; t < p.T; t += 256)
+            if (slots[t] == slot && t != row) found |= t < row ? 1 : 2;
+        const int all = (__ballot((found & 1) != 0) != 0 ? 1 : 0) | (__ballot((found & 2) != 0) != 0 ? 2 : 0);
+        if ((threadIdx.x & 63) == 0) seen[threadIdx.x >> 6] = all;
+        __syncthreads();
+        const int any = seen[0] | seen[1] | seen[2] | seen[3];
+        if (any & 1) return;
+        again = (any & 2) != 0;
     }
-    if (c >= p.C) return;
-    const float decay = decay_of(p.lam[c], p.scale);
-    const uint32_t off = (uint32_t)c * Elem<T>::kBytes;
-    float h = state[(size_t)slot * p.C + c];
-    for (int t = row; t < (slots ? p.T : row + 1); ++t) {
-        if (slots && slots[t] != slot) continue;
-        const uint64_t EB = Elem<T>::kBytes;
-        const Pack<T, 1> x = load_pack<T, 1>((uint64_t)p.x + t * p.sx * EB, off), r = load_pack<T, 1>((uint64_t)p.r + t * p.sr * EB, off),
-                         i = load_pack<T, 1>((uint64_t)p.i + t * p.si * EB, off);
-        const Gates g = gates<T, 1>(r, i, 0, decay);
-        h = fmaf(g.a, h, g.b * g.si * get<T, 1>(x, 0));
-        store_pack<T, 1>((uint64_t)p.h + t * p.sh * EB, off, &h);
+    if (keep >= V) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) decay[v] = decay_of(decay[v], p.scale);
+    for (int t = row;;) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Gates g = gates<T, V>(r, i, v, decay[v]);
+            h[v] = fmaf(g.a, h[v], g.b * g.si * get<T, V>(x, v));
+        }
+        const uint64_t to = (uint64_t)p.h + t * p.sh * EB;
+        if (keep == 0) {
+            store_pack<T, V>(to, off, h);
+        } else {
+#pragma unroll
+            for (int v = 1; v < V; ++v)
+                if (v >= keep) store_pack<T, 1>(to, off + v * (uint32_t)EB, h + v);
+        }
+        if (again)
+            do ++t; while (t < p.T && slots[t] != slot);
+        if (!again || t >= p.T) break;
+        x = load_pack<T, V>((uint64_t)p.x + t * p.sx * EB, off);
+        r = load_pack<T, V>((uint64_t)p.r + t * p.sr * EB, off);
+        i = load_pack<T, V>((uint64_t)p.i + t * p.si * EB, off);
     }
-    state[(size_t)slot * p.C + c] = h;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (v >= keep) st[v] = h[v];
 }
 
 int launched() { return hipGetLastError() == hipSuccess ? SCAN2D_OK : SCAN2D_ERR_LAUNCH_FAILED; }
@@ -717,11 +795,14 @@ int recur_bwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
 }
 
 int recur_step_launch(const scan2d_recur_desc* d, const RecurArgs& a, float* state, const int32_t* slots, long long slot_count, hipStream_t stream) {
-    const long long blocks = (long long)((a.C + 255) / 256) * a.T;
+    const int V = a.C <= 256 ? 1 : 2;                       // one channel per lane where a workgroup has the row then
+    const long long blocks = (long long)((a.C + 256 * V - 1) / (256 * V)) * a.T;
     if (!launch_fits(blocks, 256)) return SCAN2D_ERR_BAD_SHAPE;
     (void)hipGetLastError();
-    if (d->dtype == SCAN2D_BF16) hipLaunchKernelGGL(recur_step_kernel<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, stream, a, state, slots, slot_count);
-    else hipLaunchKernelGGL(recur_step_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, stream, a, state, slots, slot_count);
+    using Kernel = void (*)(const RecurArgs, float*, const int32_t*, long long);
+    const Kernel k = d->dtype == SCAN2D_BF16 ? (V == 1 ? recur_step_kernel<bf16_t, 1> : recur_step_kernel<bf16_t, 2>)
+                                             : (V == 1 ? recur_step_kernel<float, 1> : recur_step_kernel<float, 2>);
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, stream, a, state, slots, slot_count);
     return launched();
 }
 

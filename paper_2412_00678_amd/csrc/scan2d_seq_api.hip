@@ -46,7 +46,7 @@ RecurArgs recur_args(const scan2d_recur_desc* d) {
 int check_norm(const scan2d_group_norm_desc* d) {
     if (d == nullptr) return SCAN2D_ERR_NULL_POINTER;
     if (d->N < 1 || d->P < 1 || d->C < 1 || d->G < 1 || d->C >= (1 << 24) || d->C % d->G != 0) return SCAN2D_ERR_BAD_SHAPE;
-    if (d->P >= (1LL << 31) || d->P * d->N >= (1LL << 31)) return SCAN2D_ERR_BAD_SHAPE;
+    if (d->P >= (1LL << 31) || d->P * d->N >= (1LL << 31) - 4096) return SCAN2D_ERR_BAD_SHAPE;
     if (d->dtype != SCAN2D_F32 && d->dtype != SCAN2D_BF16) return SCAN2D_ERR_BAD_DTYPE;
     if (d->act != SCAN2D_ACT_NONE && d->act != SCAN2D_ACT_SILU && d->act != SCAN2D_ACT_GELU) return SCAN2D_ERR_BAD_FLAGS;
     if (!(d->eps >= 0.0f)) return SCAN2D_ERR_BAD_SHAPE;
