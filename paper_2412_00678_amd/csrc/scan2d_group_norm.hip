@@ -76,7 +76,10 @@ struct Geo {
     int lanes;                           // lanes of a row: width / V rounded up
     int slots;                           // rows a team takes at once: ts / lanes
     int tpg;                             // lanes that add up a group, a power of two
+    float per_lanes, per_D;              // 1 / lanes, 1 / D
 };
+// a / b for 0 <= a < 2^22, with 1 / b rounded: (a + 1/2) / b is at least 1 / 2b from a whole number, and off by less
+__device__ __forceinline__ int quotient(int a, float per_b) { return (int)(((float)a + 0.5f) * per_b); }
 
 // A team's slab, and this lane's channels of it.  ONE: a lane's channels are of one group (V divides the groups' channels).
 template <int V, bool ONE>
@@ -110,8 +113,8 @@ struct Lane {
             hi = lo + groups * D;
         }
         width = hi - lo;
-        slot = lane / q.lanes;
-        const int mine = lo + (lane % q.lanes) * V;
+        slot = quotient(lane, q.per_lanes);
+        const int mine = lo + (lane - slot * q.lanes) * V;
         first = mine - lo;
         on = slot < q.slots && mine < hi;
         c = min(mine, C - V);
@@ -122,7 +125,7 @@ struct Lane {
             all = all && own[v];
         }
 #pragma unroll
-        for (int v = 0; v < GV; ++v) gr[v] = min(max((ONE ? mine : c + v) - lo, 0) / D, groups - 1);
+        for (int v = 0; v < GV; ++v) gr[v] = q.spg > 1 ? 0 : min(quotient(max((ONE ? mine : c + v) - lo, 0), q.per_D), groups - 1);
     }
 };
 
@@ -308,7 +311,32 @@ __global__ __launch_bounds__(TH) void group_norm_fwd_kernel(const GroupNormArgs 
     }
 }
 
-// parts: [..][C][2], the sums for dbeta and dgamma of the items that a team, or a workgroup of teams, had.
+// parts: [..][C][2], the sums for dbeta and dgamma of the items that a team, or a workgroup of teams, had: the rows of a team, or where every
+// team has the one slab of all the workgroup's, together, channel by channel.  red: 2 TH V floats of the workgroup.
+template <int V, bool ONE, int TH, bool WAVE>
+__device__ __forceinline__ void write_parts(const GroupNormArgs& p, const Geo& q, const Lane<V, ONE>& l, int team, int teams, float* red, const float* accb,
+                                            const float* accg, float2* parts) {
+    const int tid = threadIdx.x, base = tid - l.lt;
+    const bool together = !WAVE || q.slabs == 1;
+    const int teams_here = WAVE && together ? TH / q.ts : 1, size = teams_here * q.ts * V, slot = (WAVE && together ? tid / q.ts * q.slots : 0) + l.slot;
+    float* const sums = WAVE && together ? red : red + 2 * base * V;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (l.own[v]) {
+            sums[slot * l.width + l.c + v - l.lo] = accb[v];
+            sums[size + slot * l.width + l.c + v - l.lo] = accg[v];
+        }
+    __syncthreads();
+    if (team >= teams && !together) return;
+    float2* const to = parts + (size_t)(WAVE && together ? (int)blockIdx.x : team / q.slabs) * p.C + l.lo;
+    for (int c = WAVE && together ? tid : l.lt; c < l.width; c += WAVE && together ? TH : q.ts) {
+        float b = 0.0f, g = 0.0f;
+        for (int s = 0; s < teams_here * q.slots; ++s) { b += sums[s * l.width + c]; g += sums[size + s * l.width + c]; }
+        to[c] = make_float2(b, g);
+    }
+}
+
 template <typename T, int V, bool ONE, int K, int R, int TH, bool WAVE, int ACT>
 __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs p, const Geo q, int teams, float2* parts) {
     constexpr int GV = Lane<V, ONE>::GV, PER = ONE ? 1 : V;
@@ -402,26 +430,172 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
         }
         team_sync<WAVE>();                                  // res has been read
     }
-    if (parts == nullptr) return;
-    // the rows of a team, or where every team has the one slab of all the workgroup's, together, channel by channel
-    const bool together = !WAVE || q.slabs == 1;
-    const int teams_here = WAVE && together ? TH / q.ts : 1, size = teams_here * q.ts * V, slot = (WAVE && together ? tid / q.ts * q.slots : 0) + l.slot;
-    float* const sums = WAVE && together ? red : red + 2 * base * V;
-    __syncthreads();
+    if (parts != nullptr) write_parts<V, ONE, TH, WAVE>(p, q, l, team, teams, red, accb, accg, parts);
+}
+
+// ---- single rows whose groups are a power of two of lanes: the sums stay in registers and cross the lanes by DPP and lane
+// swaps (through LDS, as above, they took as long as the memory), and the next items are asked for before these are worked on.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
+// NR sums over the `lanes` neighbours (a power of two, aligned) of each lane; all of them get them.
+template <int NR>
+__device__ __forceinline__ void lane_sums(int lanes, float (&s)[NR]) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (l.own[v]) {
-            sums[slot * l.width + l.c + v - l.lo] = accb[v];
-            sums[size + slot * l.width + l.c + v - l.lo] = accg[v];
+    for (int r = 0; r < NR; ++r)
+        if (lanes > 1) s[r] += dpp<0xB1>(s[r]);             // quad_perm 1 0 3 2
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+        if (lanes > 2) s[r] += dpp<0x4E>(s[r]);             // quad_perm 2 3 0 1
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+        if (lanes > 4) s[r] += dpp<0x141>(s[r]);            // row_half_mirror: the other quad's sum
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+        if (lanes > 8) s[r] += dpp<0x140>(s[r]);            // row_mirror: the other half row's
+    if (lanes > 16) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const auto w = __builtin_amdgcn_permlane16_swap(__float_as_int(s[r]), __float_as_int(s[r]), false, false);
+            s[r] = __int_as_float(w[0]) + __int_as_float(w[1]);
         }
-    __syncthreads();
-    if (team >= teams && !together) return;
-    float2* const to = parts + (size_t)(WAVE && together ? (int)blockIdx.x : team / q.slabs) * p.C + l.lo;
-    for (int c = WAVE && together ? tid : lt; c < l.width; c += WAVE && together ? TH : q.ts) {
-        float b = 0.0f, g = 0.0f;
-        for (int s = 0; s < teams_here * q.slots; ++s) { b += sums[s * l.width + c]; g += sums[size + s * l.width + c]; }
-        to[c] = make_float2(b, g);
     }
+    if (lanes > 32) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const auto w = __builtin_amdgcn_permlane32_swap(__float_as_int(s[r]), __float_as_int(s[r]), false, false);
+            s[r] = __int_as_float(w[0]) + __int_as_float(w[1]);
+        }
+    }
+}
+constexpr int kTokenThreads = 256;
+// R items' rows of a lane
+template <typename T, int V, int R>
+__device__ __forceinline__ void load_tokens(const GroupNormArgs& p, const void* x, long long sx, int c, long long n0, long long step, Pack<T, V>* to) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) to[i] = load_pack<T, V>(static_cast<const T*>(x) + min(n0 + i * step, (long long)p.N - 1) * sx + c);
+}
+template <typename T, int V, int R, int ACT>
+__global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const GroupNormArgs p, const Geo q, int teams) {
+    const int lt = threadIdx.x & (q.ts - 1), team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts), L = q.D / V;
+    const Lane<V, true> l(q, p.C, p.G, team % q.slabs, lt);
+    const long long step = teams / q.slabs;
+    long long n0 = team < teams ? team / q.slabs : p.N;    // none for lanes to spare
+    Pack<T, V> x[R];
+    load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0, step, x);
+    float gamma[V], beta[V];
+    load_params<V>(p, l.c, gamma, beta);
+    const float inv = 1.0f / (float)q.D;
+    for (long long it = 0; it * R * step < p.N; ++it, n0 += R * step) {
+        Pack<T, V> next[R];
+        if ((it + 1) * R * step < p.N) load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0 + R * step, step, next);
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            mean[i] = get<T, V>(x[i], 0);
+#pragma unroll
+            for (int v = 1; v < V; ++v) mean[i] += get<T, V>(x[i], v);
+        }
+        lane_sums<R>(L, mean);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            mean[i] *= inv;
+            rstd[i] = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float d = get<T, V>(x[i], v) - mean[i];
+                rstd[i] = fmaf(d, d, rstd[i]);
+            }
+        }
+        lane_sums<R>(L, rstd);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const long long n = n0 + i * step;
+            if (n < p.N && l.on) {
+                const bool out = p.mask != nullptr && p.mask[n] != 0;
+                const float m = out ? 0.0f : mean[i], rs = out ? 0.0f : 1.0f / sqrtf(rstd[i] * inv + p.eps);
+                float y[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) y[v] = out ? 0.0f : act_of<ACT>(fmaf((get<T, V>(x[i], v) - m) * rs, gamma[v], beta[v]));
+                store_pack<T, V>(static_cast<T*>(p.y) + n * p.sy + l.c, y);
+                if ((lt & (L - 1)) == 0) {
+                    float* st = p.stats + ((size_t)n * p.G + l.g0 + l.gr[0]) * 2;
+                    st[0] = m;
+                    st[1] = rs;
+                }
+            }
+            x[i] = next[i];
+        }
+    }
+}
+template <typename T, int V, int R, int ACT>
+__global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(const GroupNormArgs p, const Geo q, int teams, float2* parts) {
+    __shared__ float red[2 * kTokenThreads * V];
+    const int lt = threadIdx.x & (q.ts - 1), team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts), L = q.D / V;
+    const Lane<V, true> l(q, p.C, p.G, team % q.slabs, lt);
+    const long long step = teams / q.slabs;
+    long long n0 = team < teams ? team / q.slabs : p.N;
+    Pack<T, V> x[R], dy[R];
+    float mean[R], rstd[R];
+    const auto load_stats = [&](long long from, float* m, float* r) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float* st = p.stats + ((size_t)min(from + i * step, (long long)p.N - 1) * p.G + l.g0 + l.gr[0]) * 2;
+            m[i] = st[0];
+            r[i] = st[1];
+        }
+    };
+    load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0, step, x);
+    load_tokens<T, V, R>(p, p.dy, p.sdy, l.c, n0, step, dy);
+    load_stats(n0, mean, rstd);
+    float gamma[V], beta[V], accb[V], accg[V];
+    load_params<V>(p, l.c, gamma, beta);
+#pragma unroll
+    for (int v = 0; v < V; ++v) accb[v] = accg[v] = 0.0f;
+    const float inv = 1.0f / (float)q.D;
+    for (long long it = 0; it * R * step < p.N; ++it, n0 += R * step) {
+        Pack<T, V> nx[R], ndy[R];
+        float nmean[R], nrstd[R];
+        if ((it + 1) * R * step < p.N) {
+            load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0 + R * step, step, nx);
+            load_tokens<T, V, R>(p, p.dy, p.sdy, l.c, n0 + R * step, step, ndy);
+            load_stats(n0 + R * step, nmean, nrstd);
+        }
+        float s1[R], s2[R], dv[R][V];
+        bool live[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const long long n = n0 + i * step;
+            live[i] = n < p.N && l.on && (p.mask == nullptr || p.mask[n] == 0);
+            s1[i] = s2[i] = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float xh = (get<T, V>(x[i], v) - mean[i]) * rstd[i];
+                dv[i][v] = live[i] ? get<T, V>(dy[i], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v])) : 0.0f;
+                const float g = live[i] ? dv[i][v] * xh : 0.0f;
+                accb[v] += dv[i][v];
+                accg[v] += g;
+                s1[i] = fmaf(dv[i][v], gamma[v], s1[i]);
+                s2[i] = fmaf(g, gamma[v], s2[i]);
+            }
+        }
+        lane_sums<R>(L, s1);
+        lane_sums<R>(L, s2);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const long long n = n0 + i * step;
+            if (n < p.N && l.on) {
+                float dx[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float xh = (get<T, V>(x[i], v) - mean[i]) * rstd[i];
+                    dx[v] = live[i] ? rstd[i] * (fmaf(dv[i][v], gamma[v], -s1[i] * inv) - xh * (s2[i] * inv)) : 0.0f;
+                }
+                store_pack<T, V>(static_cast<T*>(p.dx) + n * p.sdx + l.c, dx);
+            }
+            x[i] = nx[i]; dy[i] = ndy[i]; mean[i] = nmean[i]; rstd[i] = nrstd[i];
+        }
+    }
+    if (parts != nullptr) write_parts<V, true, kTokenThreads, true>(p, q, l, team, teams, red, accb, accg, parts);
 }
 
 // dbeta and dgamma from E parts of them: 16 channels x 64 shares of the parts per workgroup, joined in order.
@@ -429,11 +603,13 @@ __device__ __forceinline__ void join_params(const float2* parts, int E, int C, f
                                             float2 (*red)[16]) {
     const int c = block * 16 + lane;
     float2 s = make_float2(0.0f, 0.0f);
-    if (c < C)
+    if (c < C) {
+#pragma unroll 8
         for (int k = share; k < E; k += shares) {
             const float2 t = parts[(size_t)k * C + c];
             s.x += t.x; s.y += t.y;
         }
+    }
     red[share][lane] = s;
     __syncthreads();
     if (share == 0 && c < C) {
@@ -448,7 +624,7 @@ __global__ __launch_bounds__(1024) void group_norm_params_kernel(const float2* p
 }
 
 // ---- split form
-constexpr int kTileThreads = 256, kRows = 8;
+constexpr int kTileThreads = 256, kRows = 4;
 struct Tile {
     long long n;
     int chunk, slab, r0, r1;             // the tile's positions
@@ -487,7 +663,8 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const Gr
 #pragma unroll
     for (int v = 0; v < V; ++v) mean[v] = m2[v] = 0.0f;
     int mine = 0;
-    for (int r = t.r0; r < t.r1; r += q.slots * kRows) {
+    const int batch = q.slots * kRows;
+    for (int r = t.r0; r < t.r1; r += batch) {
         Pack<T, V> x[kRows];
         bool live[kRows];
         load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
@@ -533,9 +710,11 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const Gr
 // The mean and rstd of a group from its E tiles, by `lanes` lanes (a power of two up to 64, neighbours) of which this is lane `l`.
 __device__ __forceinline__ float2 join_tiles(const float4* tiles, int E, float eps, int l, int lanes) {
     float M = 0.0f, s = 0.0f, m2 = 0.0f;
+#pragma unroll 8
     for (int e = l; e < E; e += lanes) { const float4 t = tiles[e]; M += t.x; s = fmaf(t.x, t.y, s); }
     for (int m = 1; m < lanes; m <<= 1) { M += __shfl_xor(M, m); s += __shfl_xor(s, m); }
     const float mean = M > 0.0f ? s / M : 0.0f;
+#pragma unroll 8
     for (int e = l; e < E; e += lanes) {
         const float4 t = tiles[e];
         const float d = t.y - mean;
@@ -558,7 +737,10 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const Gr
     const Tile t(q, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
-    const int batch = q.slots * kRows;
+    const int batch = q.slots * kRows, last = t.r0 + (t.r1 - 1 - t.r0) / batch * batch;
+    Pack<T, V> x[kRows];
+    bool live[kRows];
+    load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, last, x, live);
     float gamma[V], beta[V], mean[GV], rstd[GV];
     load_params<V>(p, l.c, gamma, beta);
     if (part != nullptr) {
@@ -580,10 +762,8 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const Gr
         rstd[v] = part != nullptr ? joined[l.gr[v]].y : st[1];
     }
     if (!l.on) return;
-    for (int r = t.r0 + (t.r1 - 1 - t.r0) / batch * batch; r >= t.r0; r -= batch) {
-        Pack<T, V> x[kRows];
-        bool live[kRows];
-        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+    for (int r = last; r >= t.r0; r -= batch) {
+        if (r < last) load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             const int at = r + l.slot + k * q.slots;
@@ -607,6 +787,11 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
     const Tile t(q, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
+    const int batch = q.slots * kRows;
+    Pack<T, V> x[kRows], dy[kRows];
+    bool live[kRows];
+    load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, t.r0, x, live);
+    load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, t.r0, dy, nullptr);
     float gamma[V], beta[V], mean[GV], rstd[GV], b[V], g[V];
     load_params<V>(p, l.c, gamma, beta);
 #pragma unroll
@@ -618,11 +803,11 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
 #pragma unroll
     for (int v = 0; v < V; ++v) b[v] = g[v] = 0.0f;
     int mine = 0;
-    for (int r = t.r0; r < t.r1; r += q.slots * kRows) {
-        Pack<T, V> x[kRows], dy[kRows];
-        bool live[kRows];
-        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
-        load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
+    for (int r = t.r0; r < t.r1; r += batch) {
+        if (r > t.r0) {
+            load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+            load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
+        }
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             mine += live[k];
@@ -670,11 +855,13 @@ __global__ __launch_bounds__(kJoinThreads) void group_norm_chan_kernel(const flo
     for (int c0 = 0; c0 < width; c0 += kJoinThreads) {      // more than one turn only for a group of more channels than threads
         const int w = min(width - c0, kJoinThreads), shares = kJoinThreads / w, c = tid % w, share = tid / w;
         float2 s = make_float2(0.0f, 0.0f);
-        if (share < shares)
+        if (share < shares) {
+#pragma unroll 8
             for (int k = share; k < chunks; k += shares) {
                 const float2 t = sums[(n * chunks + k) * C + lo + c0 + c];
                 s.x += t.x; s.y += t.y;
             }
+        }
         __syncthreads();
         red[tid] = s;
         __syncthreads();
@@ -725,7 +912,11 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const Gro
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     if (!l.on) return;
     const long long row0 = t.n * p.P;
-    const int batch = q.slots * kRows;
+    const int batch = q.slots * kRows, last = t.r0 + (t.r1 - 1 - t.r0) / batch * batch;
+    Pack<T, V> x[kRows], dy[kRows];
+    bool live[kRows];
+    load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, last, x, live);
+    load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, last, dy, nullptr);
     float gamma[V], beta[V], mean[GV], rstd[GV], s1[GV], s2[GV];
     load_params<V>(p, l.c, gamma, beta);
 #pragma unroll
@@ -736,11 +927,11 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const Gro
         s1[v] = coef[at].x;
         s2[v] = coef[at].y;
     }
-    for (int r = t.r0 + (t.r1 - 1 - t.r0) / batch * batch; r >= t.r0; r -= batch) {
-        Pack<T, V> x[kRows], dy[kRows];
-        bool live[kRows];
-        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
-        load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
+    for (int r = last; r >= t.r0; r -= batch) {
+        if (r < last) {
+            load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+            load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
+        }
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             const int at = r + l.slot + k * q.slots;
@@ -762,9 +953,10 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const Gro
 // ---- shapes
 constexpr int kMaxWgs = 2048;            // workgroups of the held form: eight per compute unit
 constexpr int kTileWgs = 1024;           // tiles of the split form, at least, where there are rows enough: four per compute unit
-enum { FORM_WAVE = 0, FORM_GROUP = 1, FORM_SPLIT = 2 };
+enum { FORM_WAVE = 0, FORM_GROUP = 1, FORM_SPLIT = 2, FORM_TOKENS = 3 };
 constexpr int kHeldRows = 8, kWaveThreads = 256, kGroupThreads = 512;
 constexpr int kItems = 4, kItemsBwd = 2;                   // single rows that a lane takes at once
+constexpr int kTokenWgs = 1024;                            // four workgroups of single rows per compute unit
 
 int floor_pow2(int v) {
     int r = 1;
@@ -801,6 +993,8 @@ bool fill_geo(const scan2d_group_norm_desc* d, int V, int ts, int most, bool who
     q->lanes = (q->width + V - 1) / V;
     if (q->lanes > ts) return false;
     q->slots = ts / q->lanes;
+    q->per_lanes = 1.0f / (float)q->lanes;
+    q->per_D = 1.0f / (float)q->D;
     q->tpg = floor_pow2(ts / (q->gps < ts ? q->gps : ts));
     if (q->tpg > 64) q->tpg = 64;
     return true;
@@ -819,6 +1013,24 @@ NormPlan plan_of(const scan2d_group_norm_desc* d) {
         n.parts = form == FORM_WAVE && n.q.slabs == 1 ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams / n.q.slabs;
         return n;
     };
+    // single rows, groups of a power of two of lanes: the widest loads that leave whole groups to a wavefront
+    for (int V = d->dtype == SCAN2D_BF16 ? 8 : 4; V >= 4 && d->P == 1; V /= 2) {
+        const int L = D / V;
+        if (D % V != 0 || L > 64 || (L & (L - 1)) != 0) continue;
+        int ts = 1;
+        while (ts < 64 && ts * V < d->C) ts *= 2;
+        if (!fill_geo(d, V, ts, ts * V, true, &n.q) || n.q.slots != 1) continue;
+        n.form = FORM_TOKENS;
+        n.V = V;
+        n.K = 1;
+        n.one = true;
+        long long most = (long long)kTokenWgs * (kTokenThreads / ts);
+        most = most < n.q.slabs ? n.q.slabs : most / n.q.slabs * n.q.slabs;
+        n.teams = (long long)d->N * n.q.slabs;
+        if (n.teams > most) n.teams = most;
+        n.parts = n.q.slabs == 1 ? (n.teams * ts + kTokenThreads - 1) / kTokenThreads : n.teams / n.q.slabs;
+        return n;
+    }
     // a team within a wavefront: the fewest lanes that hold a row's slab and all positions
     for (int ts = 1; ts <= 64; ts *= 2) {
         const int most = ts * n.V;
@@ -849,21 +1061,22 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 int launched() { return hipGetLastError() == hipSuccess ? SCAN2D_OK : SCAN2D_ERR_LAUNCH_FAILED; }
 
 template <typename T, int V, bool ONE, int ACT>
-int fwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
-    if (n.form != FORM_SPLIT) {
-        using Kernel = void (*)(const GroupNormArgs, const Geo, int);
-        const bool wave = n.form == FORM_WAVE;
-        Kernel k = wave ? group_norm_fwd_kernel<T, V, ONE, kHeldRows, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, kHeldRows, 1, kGroupThreads, false, ACT>;
-        if constexpr (V > 1)
-            if (n.K == 1) {
-                // one item per team: none that it could take besides
-                if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
-                else k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, kItems, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, kItems, kGroupThreads, false, ACT>;
-            }
-        const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
-        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams);
-        return launched();
-    }
+int fwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
+    using Kernel = void (*)(const GroupNormArgs, const Geo, int);
+    const bool wave = n.form == FORM_WAVE;
+    Kernel k = wave ? group_norm_fwd_kernel<T, V, ONE, kHeldRows, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, kHeldRows, 1, kGroupThreads, false, ACT>;
+    if constexpr (V > 1)
+        if (n.K == 1) {
+            // one item per team: none that it could take besides
+            if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
+            else k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, kItems, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, kItems, kGroupThreads, false, ACT>;
+        }
+    const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams);
+    return launched();
+}
+template <typename T, int V, bool ONE, int ACT>
+int fwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const long long blocks = (long long)a.N * n.chunks * n.q.slabs, groups = (long long)a.N * a.G;
     if (!launch_fits(blocks, kTileThreads) || !launch_fits(groups, 64)) return SCAN2D_ERR_BAD_SHAPE;
     float4* part = static_cast<float4*>(a.workspace);
@@ -875,24 +1088,27 @@ int fwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     return launched();
 }
 template <typename T, int V, bool ONE, int ACT>
-int bwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
+int bwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
     const unsigned cols = (a.C + 15) / 16;
-    if (n.form != FORM_SPLIT) {
-        using Kernel = void (*)(const GroupNormArgs, const Geo, int, float2*);
-        const bool wave = n.form == FORM_WAVE;
-        float2* parts = params ? static_cast<float2*>(a.workspace) : nullptr;
-        Kernel k = wave ? group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kGroupThreads, false, ACT>;
-        if constexpr (V > 1)
-            if (n.K == 1) {
-                if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
-                else k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kGroupThreads, false, ACT>;
-            }
-        const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
-        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams, parts);
-        if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3(cols), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
-        return launched();
-    }
+    using Kernel = void (*)(const GroupNormArgs, const Geo, int, float2*);
+    const bool wave = n.form == FORM_WAVE;
+    float2* parts = params ? static_cast<float2*>(a.workspace) : nullptr;
+    Kernel k = wave ? group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kGroupThreads, false, ACT>;
+    if constexpr (V > 1)
+        if (n.K == 1) {
+            if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
+            else k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kGroupThreads, false, ACT>;
+        }
+    const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams, parts);
+    if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3(cols), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
+    return launched();
+}
+template <typename T, int V, bool ONE, int ACT>
+int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
+    const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
+    const unsigned cols = (a.C + 15) / 16;
     const int gw = a.D >= 16 ? 1 : (16 + a.D - 1) / a.D, sets = (a.G + gw - 1) / gw;
     const long long blocks = (long long)a.N * n.chunks * n.q.slabs, joins = (long long)a.N * sets;
     if (!launch_fits(blocks + cols, kTileThreads) || !launch_fits(joins, kJoinThreads)) return SCAN2D_ERR_BAD_SHAPE;
@@ -914,6 +1130,34 @@ int bwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     return launched();
 }
 
+template <typename T, int V, bool ONE, int ACT>
+int fwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
+    if (n.form == FORM_TOKENS) {
+        if constexpr (ONE && V > 1) {
+            const long long blocks = (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads;
+            hipLaunchKernelGGL((group_norm_tokens_kernel<T, V, 16 / V, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams);
+        }
+        return launched();
+    }
+    if constexpr (V <= 4) return n.form == FORM_SPLIT ? fwd_split<T, V, ONE, ACT>(a, n, stream) : fwd_held<T, V, ONE, ACT>(a, n, stream);
+    return SCAN2D_ERR_BAD_SHAPE;                            // eight channels of a lane: single rows only
+}
+template <typename T, int V, bool ONE, int ACT>
+int bwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
+    const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
+    const unsigned cols = (a.C + 15) / 16;
+    if (n.form == FORM_TOKENS) {
+        if constexpr (ONE && V > 1) {
+            const long long blocks = (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads;
+            float2* parts = params ? static_cast<float2*>(a.workspace) : nullptr;
+            hipLaunchKernelGGL((group_norm_tokens_bwd_kernel<T, V, V == 8 ? 1 : 2, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams, parts);
+            if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3(cols), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
+        }
+        return launched();
+    }
+    if constexpr (V <= 4) return n.form == FORM_SPLIT ? bwd_split<T, V, ONE, ACT>(a, n, stream) : bwd_held<T, V, ONE, ACT>(a, n, stream);
+    return SCAN2D_ERR_BAD_SHAPE;
+}
 template <typename T, int V, bool ONE>
 int by_act(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
     (void)hipGetLastError();
@@ -926,6 +1170,8 @@ int by_act(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t
 template <typename T>
 int by_lane(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
     if (n.V == 1) return by_act<T, 1, true>(a, n, backward, stream);
+    if constexpr (sizeof(T) == 2)
+        if (n.V == 8) return by_act<T, 8, true>(a, n, backward, stream);
     return n.one ? by_act<T, 4, true>(a, n, backward, stream) : by_act<T, 4, false>(a, n, backward, stream);
 }
 int dispatch(const scan2d_group_norm_desc* d, const GroupNormArgs& a, bool backward, hipStream_t stream) {

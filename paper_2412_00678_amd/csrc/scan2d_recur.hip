@@ -28,7 +28,7 @@ namespace scan2d {
 namespace {
 
 constexpr int kTeam = 4, kTeams = 8, kGroup = kTeam * kTeams;     // chunks of a team, teams of a group
-constexpr int kSavedRows = 64;           // rows between the states that the forward saves: a chunk of the backward
+constexpr int kSavedRows = 96;           // rows between the states that the forward saves: a chunk of the backward
 
 __device__ __forceinline__ float sigmoid(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t * kLog2e)); }
 
@@ -59,10 +59,7 @@ __device__ __forceinline__ Pack<T, V> load_pack(uint64_t row, uint32_t offset) {
     Pack<T, V> r;
     if constexpr (V * Elem<T>::kBytes == 2) r.w[0] = *reinterpret_cast<__attribute__((address_space(1))) const u16_a1*>(p);
     else if constexpr (V * Elem<T>::kBytes == 4) r.w[0] = *reinterpret_cast<__attribute__((address_space(1))) const u32_a1*>(p);
-    else if constexpr (V * Elem<T>::kBytes == 16) {
-        const u32x4_a1 v = *reinterpret_cast<__attribute__((address_space(1))) const u32x4_a1*>(p);
-        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
-    } else {
+    else {
         static_assert(V * Elem<T>::kBytes == 8, "two dwords");
         const u32x2_a1 v = *reinterpret_cast<__attribute__((address_space(1))) const u32x2_a1*>(p);
         r.w[0] = v.x; r.w[1] = v.y;
@@ -71,21 +68,22 @@ __device__ __forceinline__ Pack<T, V> load_pack(uint64_t row, uint32_t offset) {
 }
 template <typename T, int V>
 __device__ __forceinline__ float get(const Pack<T, V>& r, int j) { return get_elem<T, V>(r.w, j); }
+// Outputs go past the L2's keeping (non-temporal): nothing reads them again here, and rows that are still to be read stay
+// (5003 x 771 fp32 backward 44.9 us without, 40.6 with; 16384 x 2048 bf16 153 and 142).
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(uint64_t row, uint32_t offset, const float* v) {
     const gmut p = (gmut)row + offset;
-    if constexpr (V == 1 && Elem<T>::kBytes == 2) *reinterpret_cast<__attribute__((address_space(1))) u16_a1*>(p) = (uint16_t)f32_to_bf16_bits(v[0]);
-    else if constexpr (V == 1) *reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p) = __float_as_uint(v[0]);
-    else if constexpr (V == 2 && Elem<T>::kBytes == 2) *reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p) = pack_bf16x2(v[0], v[1]);
-    else if constexpr (V * Elem<T>::kBytes == 16) {
-        u32x4_a1 w;
-        w.x = __float_as_uint(v[0]); w.y = __float_as_uint(v[1]); w.z = __float_as_uint(v[2]); w.w = __float_as_uint(v[3]);
-        *reinterpret_cast<__attribute__((address_space(1))) u32x4_a1*>(p) = w;
+    if constexpr (V * Elem<T>::kBytes == 2) {
+        __builtin_nontemporal_store((uint16_t)f32_to_bf16_bits(v[0]), reinterpret_cast<__attribute__((address_space(1))) u16_a1*>(p));
+    } else if constexpr (V * Elem<T>::kBytes == 4) {
+        uint32_t w;
+        if constexpr (V == 1) w = __float_as_uint(v[0]);
+        else w = pack_bf16x2(v[0], v[1]);
+        __builtin_nontemporal_store(w, reinterpret_cast<__attribute__((address_space(1))) u32_a1*>(p));
     } else {
         u32x2_a1 w;
-        if constexpr (Elem<T>::kBytes == 2) { w.x = pack_bf16x2(v[0], v[1]); w.y = pack_bf16x2(v[2], v[3]); }
-        else { w.x = __float_as_uint(v[0]); w.y = __float_as_uint(v[1]); }
-        *reinterpret_cast<__attribute__((address_space(1))) u32x2_a1*>(p) = w;
+        w.x = __float_as_uint(v[0]); w.y = __float_as_uint(v[1]);
+        __builtin_nontemporal_store(w, reinterpret_cast<__attribute__((address_space(1))) u32x2_a1*>(p));
     }
 }
 
@@ -266,7 +264,7 @@ __device__ __forceinline__ void chain_wait(const uint64_t* w, uint64_t* v) {
             all = all && is_set(v[q]);
         }
         if (__all(all)) return;
-        __builtin_amdgcn_s_sleep(1);
+        __builtin_amdgcn_s_sleep(4);
     }
 }
 // The value in front of chunk k (in the order of the scan) for this lane's channels, where the map of chunk k itself is (A, S);
@@ -304,7 +302,7 @@ __device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int co
                     }
                 }
             all = __all(all);
-            if (!all) __builtin_amdgcn_s_sleep(1);
+            if (!all) __builtin_amdgcn_s_sleep(4);
         }
         float tA[V], tS[V];
 #pragma unroll
@@ -635,17 +633,19 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
     }
 }
 
-// dlam from the chunks' sums: 64 channels x 16 parts of the chunks per workgroup, the parts joined in order.
+// dlam from the chunks' sums: 16 channels x 64 shares of the chunks per workgroup, the shares joined in order.
 __global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* parts, int n, int C, const float* lam, float* dlam) {
-    __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    __shared__ float red[64][16];
+    const int lane = threadIdx.x & 15, share = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
     float sum = 0.0f;
-    if (c < C)
-        for (int k = w; k < n; k += 16) sum += parts[(size_t)k * C + c];
-    red[w][lane] = sum;
+    if (c < C) {
+#pragma unroll 8
+        for (int k = share; k < n; k += 64) sum += parts[(size_t)k * C + c];
+    }
+    red[share][lane] = sum;
     __syncthreads();
-    if (w == 0 && c < C) {
-        for (int q = 1; q < 16; ++q) sum += red[q][lane];
+    if (share == 0 && c < C) {
+        for (int q = 1; q < 64; ++q) sum += red[q][lane];
         dlam[c] = sum * decay_slope(lam[c]);
     }
 }
@@ -719,18 +719,22 @@ __global__ __launch_bounds__(256) void recur_step_kernel(const RecurArgs p, floa
 int launched() { return hipGetLastError() == hipSuccess ? SCAN2D_OK : SCAN2D_ERR_LAUNCH_FAILED; }
 
 // ---- shapes.  One lane per channel up to 64 channels, two channels per lane beyond.
-constexpr int kWaves = 8;                // wavefronts of a workgroup
-constexpr int kFwdRowsF32 = 8, kFwdRowsBf16 = 16, kBwdRows = kSavedRows / kWaves;      // rows of a wavefront
+constexpr int kFwdWaves = 8, kBwdWaves = 12;                            // wavefronts of a workgroup
+constexpr int kBwdRows = kSavedRows / kBwdWaves;                       // rows of a wavefront in the backward pass
 struct RecurPlan {
     int V, chunks, cols;
-    int rows;                            // of a chunk
+    int rows, waves;                     // rows of a wavefront, wavefronts of a workgroup
 };
 RecurPlan plan_of(const scan2d_recur_desc* d, int pass) {
     RecurPlan q;
     q.V = d->C <= 64 ? 1 : 2;
-    q.rows = (pass == SCAN2D_PASS_BWD ? kBwdRows : d->dtype == SCAN2D_BF16 ? kFwdRowsBf16 : kFwdRowsF32) * kWaves;
-    q.chunks = (int)((d->T + q.rows - 1) / q.rows);
     q.cols = (d->C + 64 * q.V - 1) / (64 * q.V);
+    q.waves = pass == SCAN2D_PASS_BWD ? kBwdWaves : kFwdWaves;
+    const auto chunks = [&](int rows) { return (d->T + rows * q.waves - 1) / (rows * q.waves); };
+    // forward, bf16: 16 rows of a wavefront (9001 x 1024 30 us, with 8 rows 37), but 8 where that leaves compute units without a
+    // workgroup (1000 x 512 10.1 us, with 16 rows 12.0; 37 x 256 5.8 and 8.9)
+    q.rows = pass == SCAN2D_PASS_BWD ? kBwdRows : d->dtype == SCAN2D_BF16 && chunks(16) * q.cols >= 256 ? 16 : 8;
+    q.chunks = (int)chunks(q.rows);
     return q;
 }
 size_t chain_bytes(const RecurPlan& q) { return q.chunks > 1 ? (chain_words(q.chunks, q.cols, 64 * q.V) * 8 + 255) / 256 * 256 : 0; }
@@ -741,7 +745,7 @@ int clear_chain(const RecurPlan& q, void* workspace, hipStream_t stream) {
     return launched();
 }
 bool plan_fits(const RecurPlan& q) {
-    return launch_fits((long long)q.chunks * q.cols, 64 * kWaves) && launch_fits((long long)(chain_bytes(q) / 4096 + 1), 256);
+    return launch_fits((long long)q.chunks * q.cols, 64 * q.waves) && launch_fits((long long)(chain_bytes(q) / 4096 + 1), 256);
 }
 
 int launch_none(const RecurArgs& a, const float* from, float* to, float* zero, hipStream_t stream) {
@@ -769,9 +773,11 @@ int recur_fwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
         if (rc != SCAN2D_OK) return rc;
     }
     using Kernel = void (*)(const RecurArgs, int, int);
-    const Kernel k = d->dtype == SCAN2D_BF16 ? (q.V == 1 ? recur_fwd_kernel<bf16_t, 1, kFwdRowsBf16, kWaves> : recur_fwd_kernel<bf16_t, 2, kFwdRowsBf16, kWaves>)
-                                             : (q.V == 1 ? recur_fwd_kernel<float, 1, kFwdRowsF32, kWaves> : recur_fwd_kernel<float, 2, kFwdRowsF32, kWaves>);
-    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * kWaves), 0, stream, a, q.chunks, q.cols);
+    Kernel k;
+    if (d->dtype != SCAN2D_BF16) k = q.V == 1 ? recur_fwd_kernel<float, 1, 8, kFwdWaves> : recur_fwd_kernel<float, 2, 8, kFwdWaves>;
+    else if (q.rows == 8) k = q.V == 1 ? recur_fwd_kernel<bf16_t, 1, 8, kFwdWaves> : recur_fwd_kernel<bf16_t, 2, 8, kFwdWaves>;
+    else k = q.V == 1 ? recur_fwd_kernel<bf16_t, 1, 16, kFwdWaves> : recur_fwd_kernel<bf16_t, 2, 16, kFwdWaves>;
+    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * q.waves), 0, stream, a, q.chunks, q.cols);
     return launched();
 }
 
@@ -786,11 +792,11 @@ int recur_bwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
         if (rc != SCAN2D_OK) return rc;
     }
     using Kernel = void (*)(const RecurArgs, float*, int, int);
-    const Kernel k = d->dtype == SCAN2D_BF16 ? (q.V == 1 ? recur_bwd_kernel<bf16_t, 1, kBwdRows, kWaves> : recur_bwd_kernel<bf16_t, 2, kBwdRows, kWaves>)
-                                             : (q.V == 1 ? recur_bwd_kernel<float, 1, kBwdRows, kWaves> : recur_bwd_kernel<float, 2, kBwdRows, kWaves>);
-    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * kWaves), 0, stream, a, parts, q.chunks, q.cols);
+    const Kernel k = d->dtype == SCAN2D_BF16 ? (q.V == 1 ? recur_bwd_kernel<bf16_t, 1, kBwdRows, kBwdWaves> : recur_bwd_kernel<bf16_t, 2, kBwdRows, kBwdWaves>)
+                                             : (q.V == 1 ? recur_bwd_kernel<float, 1, kBwdRows, kBwdWaves> : recur_bwd_kernel<float, 2, kBwdRows, kBwdWaves>);
+    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * q.waves), 0, stream, a, parts, q.chunks, q.cols);
     if (q.chunks > 1)
-        hipLaunchKernelGGL(recur_dlam_kernel, dim3((a.C + 63) / 64), dim3(1024), 0, stream, parts, q.chunks, a.C, a.lam, a.dlam);
+        hipLaunchKernelGGL(recur_dlam_kernel, dim3((a.C + 15) / 16), dim3(1024), 0, stream, parts, q.chunks, a.C, a.lam, a.dlam);
     return launched();
 }
 
