@@ -34,24 +34,57 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
 }
 template <typename T, int V>
 __device__ __forceinline__ float get(const Pack<T, V>& r, int j) { return get_elem<T, V>(r.w, j); }
+// Outputs are stored non-temporally: nothing reads them again here, and what is read twice stays in the L2 (16384 tokens x 2048 bf16
+// forward 36.8 us without, 30.8 with; 2 x 9000 x 771 fp32 40.8 and 37.0).
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T* p, const float* v) {
-    if constexpr (Elem<T>::kBytes == 4) store_words_any<V>(p, reinterpret_cast<const uint32_t*>(v));
-    else if constexpr (V == 1) p->bits = (uint16_t)f32_to_bf16_bits(v[0]);
-    else {
-        uint32_t w[V / 2];
+    if constexpr (V == 1) {
+        store_elem(p, v[0]);
+    } else {
+        constexpr int W = V * Elem<T>::kBytes / 4;
+        uint32_t w[W];
 #pragma unroll
-        for (int k = 0; k < V / 2; ++k) w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
-        store_words_any<V / 2>(p, w);
+        for (int k = 0; k < W; ++k) {
+            if constexpr (Elem<T>::kBytes == 4) w[k] = __float_as_uint(v[k]);
+            else w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+        }
+        if constexpr (W == 4) {
+            u32x4_a1 q;
+            q.x = w[0]; q.y = w[1]; q.z = w[2]; q.w = w[3];
+            __builtin_nontemporal_store(q, reinterpret_cast<u32x4_a1*>(p));
+        } else {
+            static_assert(W == 2, "two or four dwords");
+            u32x2_a1 q;
+            q.x = w[0]; q.y = w[1];
+            __builtin_nontemporal_store(q, reinterpret_cast<u32x2_a1*>(p));
+        }
     }
 }
 
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
+// The normal distribution Phi(v) and e^(-v^2/2): with x = |v| / sqrt(2) and t = 1 / (1 + 0.3 x), Phi(-|v|) = t q(t) e^(-x^2) / 2, q the
+// Chebyshev fit of degree 8 to e^(x^2) erfc(x) / t (off by 3.2e-8); one exponential for Phi and its slope, a third of erff's work.
+__device__ __forceinline__ float normal_cdf(float v, float& e) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.212132034f, fabsf(v), 1.0f));
+    e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * v * v);
+    float q = fmaf(t, -0.12841005623340607f, 0.48013120889663696f);
+    q = fmaf(t, q, -0.5010061860084534f);
+    q = fmaf(t, q, 0.5347656011581421f);
+    q = fmaf(t, q, -0.08565600961446762f);
+    q = fmaf(t, q, 0.2110726535320282f);
+    q = fmaf(t, q, 0.14933134615421295f);
+    q = fmaf(t, q, 0.17057515680789948f);
+    q = fmaf(t, q, 0.16919629275798798f);
+    const float tail = 0.5f * t * q * e;
+    return v < 0.0f ? tail : 1.0f - tail;
+}
 template <int ACT>
 __device__ __forceinline__ float act_of(float v) {
     if constexpr (ACT == SCAN2D_ACT_SILU) return v * sigmoid(v);
-    else if constexpr (ACT == SCAN2D_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678f));
-    else return v;
+    else if constexpr (ACT == SCAN2D_ACT_GELU) {
+        float e;
+        return v * normal_cdf(v, e);
+    } else return v;
 }
 template <int ACT>
 __device__ __forceinline__ float act_slope(float v) {
@@ -59,7 +92,9 @@ __device__ __forceinline__ float act_slope(float v) {
         const float s = sigmoid(v);
         return s * fmaf(v, 1.0f - s, 1.0f);
     } else if constexpr (ACT == SCAN2D_ACT_GELU) {
-        return fmaf(v * 0.39894228f, __builtin_amdgcn_exp2f(-0.5f * kLog2e * v * v), 0.5f * (1.0f + erff(v * 0.70710678f)));
+        float e;
+        const float cdf = normal_cdf(v, e);
+        return fmaf(v * 0.39894228f, e, cdf);
     } else {
         return 1.0f;
     }
@@ -313,8 +348,8 @@ __global__ __launch_bounds__(TH) void group_norm_fwd_kernel(const GroupNormArgs 
 
 // parts: [..][C][2], the sums for dbeta and dgamma of the items that a team, or a workgroup of teams, had: the rows of a team, or where every
 // team has the one slab of all the workgroup's, together, channel by channel.  red: 2 TH V floats of the workgroup.
-template <int V, bool ONE, int TH, bool WAVE>
-__device__ __forceinline__ void write_parts(const GroupNormArgs& p, const Geo& q, const Lane<V, ONE>& l, int team, int teams, float* red, const float* accb,
+template <int V, int TH, bool WAVE, typename L>
+__device__ __forceinline__ void write_parts(const GroupNormArgs& p, const Geo& q, const L& l, int team, int teams, float* red, const float* accb,
                                             const float* accg, float2* parts) {
     const int tid = threadIdx.x, base = tid - l.lt;
     const bool together = !WAVE || q.slabs == 1;
@@ -430,11 +465,12 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
         }
         team_sync<WAVE>();                                  // res has been read
     }
-    if (parts != nullptr) write_parts<V, ONE, TH, WAVE>(p, q, l, team, teams, red, accb, accg, parts);
+    if (parts != nullptr) write_parts<V, TH, WAVE>(p, q, l, team, teams, red, accb, accg, parts);
 }
 
-// ---- single rows whose groups are a power of two of lanes: the sums stay in registers and cross the lanes by DPP and lane
-// swaps (through LDS, as above, they took as long as the memory), and the next items are asked for before these are worked on.
+// ---- single rows of up to 64 V channels a group: a group has a power of two of neighbouring lanes (some may be idle), the sums stay in
+// registers and cross the lanes by DPP and lane swaps (through LDS, as above, they took as long as the memory), and the
+// next items are asked for before these are worked on.
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
 // NR sums over the `lanes` neighbours (a power of two, aligned) of each lane; all of them get them.
@@ -468,16 +504,53 @@ __device__ __forceinline__ void lane_sums(int lanes, float (&s)[NR]) {
     }
 }
 constexpr int kTokenThreads = 256;
+// q.lanes: lanes of a group, a power of two; q.gps, q.slabs: groups of a team, teams of a row.  ONE: V divides a group's channels.
+template <int V, bool ONE>
+struct TokenLane {
+    int lt, slot, c, lo, width, g;       // first channel, the team's channels, the lane's group
+    bool on, first;                      // has channels; has the group's first
+    bool own[V];
+    bool all;
+    __device__ TokenLane(const Geo& q, int C, int G, int slab, int lane) {
+        lt = lane;
+        slot = 0;
+        const int g0 = slab * q.gps, at = lane / q.lanes, i = lane & (q.lanes - 1);
+        lo = g0 * q.D;
+        width = min(q.gps, G - g0) * q.D;
+        on = at < q.gps && g0 + at < G && i * V < q.D;
+        g = min(g0 + at, G - 1);
+        first = on && i == 0;
+        const int mine = g * q.D + i * V;
+        c = min(mine, C - V);
+        all = true;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            own[v] = ONE ? on : on && c + v >= mine && c + v < (g + 1) * q.D;
+            all = all && own[v];
+        }
+    }
+};
 // R items' rows of a lane
 template <typename T, int V, int R>
 __device__ __forceinline__ void load_tokens(const GroupNormArgs& p, const void* x, long long sx, int c, long long n0, long long step, Pack<T, V>* to) {
 #pragma unroll
     for (int i = 0; i < R; ++i) to[i] = load_pack<T, V>(static_cast<const T*>(x) + min(n0 + i * step, (long long)p.N - 1) * sx + c);
 }
-template <typename T, int V, int R, int ACT>
+template <typename T, int V, bool ONE>
+__device__ __forceinline__ void store_token(void* to, long long at, const TokenLane<V, ONE>& l, const float* v) {
+    T* const p = static_cast<T*>(to) + at + l.c;
+    if (ONE || l.all) {
+        store_pack<T, V>(p, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (l.own[k]) store_elem(p + k, v[k]);
+    }
+}
+template <typename T, int V, bool ONE, int R, int ACT>
 __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const GroupNormArgs p, const Geo q, int teams) {
-    const int lt = threadIdx.x & (q.ts - 1), team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts), L = q.D / V;
-    const Lane<V, true> l(q, p.C, p.G, team % q.slabs, lt);
+    const int team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts);
+    const TokenLane<V, ONE> l(q, p.C, p.G, team % q.slabs, threadIdx.x & (q.ts - 1));
     const long long step = teams / q.slabs;
     long long n0 = team < teams ? team / q.slabs : p.N;    // none for lanes to spare
     Pack<T, V> x[R];
@@ -491,22 +564,22 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const 
         float mean[R], rstd[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            mean[i] = get<T, V>(x[i], 0);
+            mean[i] = 0.0f;
 #pragma unroll
-            for (int v = 1; v < V; ++v) mean[i] += get<T, V>(x[i], v);
+            for (int v = 0; v < V; ++v) mean[i] += l.own[v] ? get<T, V>(x[i], v) : 0.0f;
         }
-        lane_sums<R>(L, mean);
+        lane_sums<R>(q.lanes, mean);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             mean[i] *= inv;
             rstd[i] = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float d = get<T, V>(x[i], v) - mean[i];
+                const float d = l.own[v] ? get<T, V>(x[i], v) - mean[i] : 0.0f;
                 rstd[i] = fmaf(d, d, rstd[i]);
             }
         }
-        lane_sums<R>(L, rstd);
+        lane_sums<R>(q.lanes, rstd);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const long long n = n0 + i * step;
@@ -516,9 +589,9 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const 
                 float y[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) y[v] = out ? 0.0f : act_of<ACT>(fmaf((get<T, V>(x[i], v) - m) * rs, gamma[v], beta[v]));
-                store_pack<T, V>(static_cast<T*>(p.y) + n * p.sy + l.c, y);
-                if ((lt & (L - 1)) == 0) {
-                    float* st = p.stats + ((size_t)n * p.G + l.g0 + l.gr[0]) * 2;
+                store_token<T, V, ONE>(p.y, n * p.sy, l, y);
+                if (l.first) {
+                    float* st = p.stats + ((size_t)n * p.G + l.g) * 2;
                     st[0] = m;
                     st[1] = rs;
                 }
@@ -527,11 +600,11 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const 
         }
     }
 }
-template <typename T, int V, int R, int ACT>
+template <typename T, int V, bool ONE, int R, int ACT>
 __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(const GroupNormArgs p, const Geo q, int teams, float2* parts) {
     __shared__ float red[2 * kTokenThreads * V];
-    const int lt = threadIdx.x & (q.ts - 1), team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts), L = q.D / V;
-    const Lane<V, true> l(q, p.C, p.G, team % q.slabs, lt);
+    const int team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts);
+    const TokenLane<V, ONE> l(q, p.C, p.G, team % q.slabs, threadIdx.x & (q.ts - 1));
     const long long step = teams / q.slabs;
     long long n0 = team < teams ? team / q.slabs : p.N;
     Pack<T, V> x[R], dy[R];
@@ -539,7 +612,7 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(co
     const auto load_stats = [&](long long from, float* m, float* r) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const float* st = p.stats + ((size_t)min(from + i * step, (long long)p.N - 1) * p.G + l.g0 + l.gr[0]) * 2;
+            const float* st = p.stats + ((size_t)min(from + i * step, (long long)p.N - 1) * p.G + l.g) * 2;
             m[i] = st[0];
             r[i] = st[1];
         }
@@ -569,17 +642,18 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(co
             s1[i] = s2[i] = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
+                const bool counts = ONE ? live[i] : live[i] && l.own[v];
                 const float xh = (get<T, V>(x[i], v) - mean[i]) * rstd[i];
-                dv[i][v] = live[i] ? get<T, V>(dy[i], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v])) : 0.0f;
-                const float g = live[i] ? dv[i][v] * xh : 0.0f;
+                dv[i][v] = counts ? get<T, V>(dy[i], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v])) : 0.0f;
+                const float g = counts ? dv[i][v] * xh : 0.0f;
                 accb[v] += dv[i][v];
                 accg[v] += g;
                 s1[i] = fmaf(dv[i][v], gamma[v], s1[i]);
                 s2[i] = fmaf(g, gamma[v], s2[i]);
             }
         }
-        lane_sums<R>(L, s1);
-        lane_sums<R>(L, s2);
+        lane_sums<R>(q.lanes, s1);
+        lane_sums<R>(q.lanes, s2);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const long long n = n0 + i * step;
@@ -590,12 +664,12 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(co
                     const float xh = (get<T, V>(x[i], v) - mean[i]) * rstd[i];
                     dx[v] = live[i] ? rstd[i] * (fmaf(dv[i][v], gamma[v], -s1[i] * inv) - xh * (s2[i] * inv)) : 0.0f;
                 }
-                store_pack<T, V>(static_cast<T*>(p.dx) + n * p.sdx + l.c, dx);
+                store_token<T, V, ONE>(p.dx, n * p.sdx, l, dx);
             }
             x[i] = nx[i]; dy[i] = ndy[i]; mean[i] = nmean[i]; rstd[i] = nrstd[i];
         }
     }
-    if (parts != nullptr) write_parts<V, true, kTokenThreads, true>(p, q, l, team, teams, red, accb, accg, parts);
+    if (parts != nullptr) write_parts<V, kTokenThreads, true>(p, q, l, team, teams, red, accb, accg, parts);
 }
 
 // dbeta and dgamma from E parts of them: 16 channels x 64 shares of the parts per workgroup, joined in order.
@@ -624,7 +698,7 @@ __global__ __launch_bounds__(1024) void group_norm_params_kernel(const float2* p
 }
 
 // ---- split form
-constexpr int kTileThreads = 256, kRows = 4;
+constexpr int kTileThreads = 512, kRows = 4;
 struct Tile {
     long long n;
     int chunk, slab, r0, r1;             // the tile's positions
@@ -952,7 +1026,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const Gro
 
 // ---- shapes
 constexpr int kMaxWgs = 2048;            // workgroups of the held form: eight per compute unit
-constexpr int kTileWgs = 1024;           // tiles of the split form, at least, where there are rows enough: four per compute unit
+constexpr int kTileWgs = 512;            // tiles of the split form, at least, where there are rows enough: two per compute unit
 enum { FORM_WAVE = 0, FORM_GROUP = 1, FORM_SPLIT = 2, FORM_TOKENS = 3 };
 constexpr int kHeldRows = 8, kWaveThreads = 256, kGroupThreads = 512;
 constexpr int kItems = 4, kItemsBwd = 2;                   // single rows that a lane takes at once
@@ -1013,22 +1087,27 @@ NormPlan plan_of(const scan2d_group_norm_desc* d) {
         n.parts = form == FORM_WAVE && n.q.slabs == 1 ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams / n.q.slabs;
         return n;
     };
-    // single rows, groups of a power of two of lanes: the widest loads that leave whole groups to a wavefront
-    for (int V = d->dtype == SCAN2D_BF16 ? 8 : 4; V >= 4 && d->P == 1; V /= 2) {
-        const int L = D / V;
-        if (D % V != 0 || L > 64 || (L & (L - 1)) != 0) continue;
-        int ts = 1;
-        while (ts < 64 && ts * V < d->C) ts *= 2;
-        if (!fill_geo(d, V, ts, ts * V, true, &n.q) || n.q.slots != 1) continue;
+    // single rows: the widest loads, and as many groups to a wavefront as it has lanes for
+    const int TV = d->dtype == SCAN2D_BF16 && D >= 8 ? 8 : 4;
+    if (d->P == 1 && d->C >= 4 && D <= 64 * TV) {
         n.form = FORM_TOKENS;
-        n.V = V;
+        n.V = TV;
         n.K = 1;
-        n.one = true;
-        long long most = (long long)kTokenWgs * (kTokenThreads / ts);
+        n.one = D % TV == 0;
+        n.q = Geo();
+        n.q.D = D;
+        n.q.lanes = 1;
+        while (n.q.lanes * TV < D) n.q.lanes *= 2;
+        n.q.ts = n.q.lanes;
+        while (n.q.ts < 64 && n.q.ts / n.q.lanes < d->G) n.q.ts *= 2;
+        n.q.gps = n.q.ts / n.q.lanes;
+        n.q.slabs = (d->G + n.q.gps - 1) / n.q.gps;
+        n.q.slots = n.q.spg = 1;
+        long long most = (long long)kTokenWgs * (kTokenThreads / n.q.ts);
         most = most < n.q.slabs ? n.q.slabs : most / n.q.slabs * n.q.slabs;
         n.teams = (long long)d->N * n.q.slabs;
         if (n.teams > most) n.teams = most;
-        n.parts = n.q.slabs == 1 ? (n.teams * ts + kTokenThreads - 1) / kTokenThreads : n.teams / n.q.slabs;
+        n.parts = n.q.slabs == 1 ? (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads : n.teams / n.q.slabs;
         return n;
     }
     // a team within a wavefront: the fewest lanes that hold a row's slab and all positions
@@ -1133,9 +1212,9 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
 template <typename T, int V, bool ONE, int ACT>
 int fwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     if (n.form == FORM_TOKENS) {
-        if constexpr (ONE && V > 1) {
+        if constexpr (V > 1) {
             const long long blocks = (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads;
-            hipLaunchKernelGGL((group_norm_tokens_kernel<T, V, 16 / V, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams);
+            hipLaunchKernelGGL((group_norm_tokens_kernel<T, V, ONE, 16 / V, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams);
         }
         return launched();
     }
@@ -1147,10 +1226,10 @@ int bwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
     const unsigned cols = (a.C + 15) / 16;
     if (n.form == FORM_TOKENS) {
-        if constexpr (ONE && V > 1) {
+        if constexpr (V > 1) {
             const long long blocks = (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads;
             float2* parts = params ? static_cast<float2*>(a.workspace) : nullptr;
-            hipLaunchKernelGGL((group_norm_tokens_bwd_kernel<T, V, V == 8 ? 1 : 2, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams, parts);
+            hipLaunchKernelGGL((group_norm_tokens_bwd_kernel<T, V, ONE, V == 8 ? 1 : 2, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams, parts);
             if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3(cols), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
         }
         return launched();
@@ -1171,7 +1250,7 @@ template <typename T>
 int by_lane(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
     if (n.V == 1) return by_act<T, 1, true>(a, n, backward, stream);
     if constexpr (sizeof(T) == 2)
-        if (n.V == 8) return by_act<T, 8, true>(a, n, backward, stream);
+        if (n.V == 8) return n.one ? by_act<T, 8, true>(a, n, backward, stream) : by_act<T, 8, false>(a, n, backward, stream);
     return n.one ? by_act<T, 4, true>(a, n, backward, stream) : by_act<T, 4, false>(a, n, backward, stream);
 }
 int dispatch(const scan2d_group_norm_desc* d, const GroupNormArgs& a, bool backward, hipStream_t stream) {
