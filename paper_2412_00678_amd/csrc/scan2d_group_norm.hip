@@ -1073,7 +1073,7 @@ bool fill_geo(const scan2d_group_norm_desc* d, int V, int ts, int most, bool who
     if (q->tpg > 64) q->tpg = 64;
     return true;
 }
-NormPlan plan_of(const scan2d_group_norm_desc* d) {
+NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
     NormPlan n = {};
     n.V = d->C >= 4 ? 4 : 1;
     const int D = d->C / d->G;
@@ -1104,8 +1104,11 @@ NormPlan plan_of(const scan2d_group_norm_desc* d) {
         n.q.slabs = (d->G + n.q.gps - 1) / n.q.gps;
         n.q.slots = n.q.spg = 1;
         long long most = (long long)kTokenWgs * (kTokenThreads / n.q.ts);
-        most = most < n.q.slabs ? n.q.slabs : most / n.q.slabs * n.q.slabs;
         n.teams = (long long)d->N * n.q.slabs;
+        // backward: at least four items a team while that leaves every SIMD a wavefront, for fewer parts of the parameters'
+        // sums (4096 tokens x 600 fp32 18.8 us without, 15.8 with; 300 x 2048 11.7 and 9.5)
+        if (backward && most > n.teams / 4) most = n.teams / 4 > 1024 ? n.teams / 4 : 1024;
+        most = most < n.q.slabs ? n.q.slabs : most / n.q.slabs * n.q.slabs;
         if (n.teams > most) n.teams = most;
         n.parts = n.q.slabs == 1 ? (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads : n.teams / n.q.slabs;
         return n;
@@ -1254,14 +1257,14 @@ int by_lane(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_
     return n.one ? by_act<T, 4, true>(a, n, backward, stream) : by_act<T, 4, false>(a, n, backward, stream);
 }
 int dispatch(const scan2d_group_norm_desc* d, const GroupNormArgs& a, bool backward, hipStream_t stream) {
-    const NormPlan n = plan_of(d);
+    const NormPlan n = plan_of(d, backward);
     return d->dtype == SCAN2D_BF16 ? by_lane<bf16_t>(a, n, backward, stream) : by_lane<float>(a, n, backward, stream);
 }
 
 }  // namespace
 
 size_t group_norm_workspace_bytes(const scan2d_group_norm_desc* d, int pass) {
-    const NormPlan n = plan_of(d);
+    const NormPlan n = plan_of(d, pass == SCAN2D_PASS_BWD);
     if (n.form != FORM_SPLIT) return pass == SCAN2D_PASS_BWD ? (size_t)n.parts * d->C * sizeof(float2) : 0;
     const size_t items = (size_t)d->N * n.chunks;
     if (pass == SCAN2D_PASS_FWD) return items * n.q.spg * d->G * sizeof(float4);

@@ -267,27 +267,27 @@ __device__ __forceinline__ void chain_wait(const uint64_t* w, uint64_t* v) {
         __builtin_amdgcn_s_sleep(4);
     }
 }
-// The value in front of chunk k (in the order of the scan) for this lane's channels, where the map of chunk k itself is (A, S);
-// every wavefront gets it.  kTeam chunks make a team, kTeams teams a group.  A chunk reads the maps of its team in front of
-// it (the first wavefront, at most 3), those of the group's teams in front of that (one for each further wavefront, at most 7) and
-// the state behind the group before (the last wavefront): 6 reads on average.  These reads pass by the L2 and count: with one level of 32
-// chunks (16 reads, the state by every wavefront) 65536 x 2048 bf16 took 287 us forward, without any 221.
+// The value in front of chunk k (in the order of the scan) for this lane's channels, where the map of chunk k itself is (A, S)
+// (of the first wavefront; the others need not have it); every wavefront gets it.  kTeam chunks make a team, kTeams teams a group.  A chunk
+// reads the maps of its team in front of it (the first wavefront, at most 3), those of the group's teams in front of that (one for
+// each further wavefront, at most 7) and the state behind the group before (the last wavefront): 6 reads on average.
 // The map of a team does not wait for other teams, nor that of a chunk for anything, so only the states, one per group, are a chain.
+// What is left is the way of two words through memory, some 4 us of a workgroup's 13: 65536 x 2048 bf16 forward takes 260 us, 218
+// without this function.  (More rows on the way meanwhile need registers that are not there: a workgroup that asks for its next
+// chunk's rows before it waits spills; one level of 32 chunks, 16 reads each, takes as long.)
 template <int V, int NW>
 __device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int col, int k, const float* A, const float* S, float* carry, ChainLds<V, NW>& lds) {
     constexpr int WIDTH = 64 * V;
-    static_assert(NW >= kTeams, "a wavefront for each team");
+    static_assert(NW > kTeams - 1, "a wavefront for each team");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int g = k / kGroup, j = k % kGroup, team = j / kTeam, q = j % kTeam;
     uint64_t* maps = ws + chain_counters(cols) + (size_t)col * WIDTH + lane;
     uint64_t* states = maps + (size_t)chunks * cols * WIDTH;
     const size_t step = (size_t)cols * WIDTH;
     const bool end = j == kGroup - 1 || k == chunks - 1;    // nobody reads the map of a group's last chunk
-    if (wave == 0) {
-        if (!end && q != kTeam - 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) chain_put(maps + (size_t)k * step + v * 64, chain_word(A[v], S[v]));
-        }
+    const bool teller = !end && q == kTeam - 1;             // the last chunk of a team: others wait for the team's map
+    // the first wavefront: the maps of the team in front of this chunk, to LDS
+    const auto near = [&] {
         uint64_t w[kTeam - 1][V];
         for (bool all = false; !all;) {
             all = true;
@@ -304,21 +304,30 @@ __device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int co
             all = __all(all);
             if (!all) __builtin_amdgcn_s_sleep(4);
         }
-        float tA[V], tS[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            tA[v] = 1.0f;
-            tS[v] = 0.0f;
+            float tA = 1.0f, tS = 0.0f;
 #pragma unroll
             for (int m = 0; m < kTeam - 1; ++m) {
                 const float a = __uint_as_float((uint32_t)(w[m][v] >> 32));
-                tS[v] = apply(a, tS[v], __uint_as_float((uint32_t)w[m][v]));
-                tA[v] = compose(tA[v], a);
+                tS = apply(a, tS, __uint_as_float((uint32_t)w[m][v]));
+                tA = compose(tA, a);
             }
-            lds.A[0][lane * V + v] = tA[v];
-            lds.S[0][lane * V + v] = tS[v];
-            if (!end && q == kTeam - 1) chain_put(maps + (size_t)k * step + v * 64, chain_word(compose(tA[v], A[v]), apply(A[v], tS[v], S[v])));
+            lds.A[0][lane * V + v] = tA;
+            lds.S[0][lane * V + v] = tS;
+            if (teller) chain_put(maps + (size_t)k * step + v * 64, chain_word(compose(tA, A[v]), apply(A[v], tS, S[v])));
         }
+    };
+    if (wave == 0) {
+        if (teller) {
+            near();
+        } else if (!end) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) chain_put(maps + (size_t)k * step + v * 64, chain_word(A[v], S[v]));
+        }
+    }
+    if (wave == 0) {
+        if (!teller) near();
     } else if (wave <= team) {
         uint64_t w[V];
         chain_wait<V>(maps + (size_t)(g * kGroup + wave * kTeam - 1) * step, w);
@@ -447,15 +456,15 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; }
     __syncthreads();
     if (chunks > 1) {
+        if (wave == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) { A[v] = 1.0f; S[v] = 0.0f; }
+            for (int w = 1; w < NW; ++w)
 #pragma unroll
-        for (int w = 0; w < NW; ++w)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                S[v] = apply(mapA[w][lane * V + v], S[v], mapS[w][lane * V + v]);
-                A[v] = compose(A[v], mapA[w][lane * V + v]);
-            }
+                for (int v = 0; v < V; ++v) {
+                    S[v] = apply(mapA[w][lane * V + v], S[v], mapS[w][lane * V + v]);
+                    A[v] = compose(A[v], mapA[w][lane * V + v]);
+                }
+        }
         chain<V, NW>(ws, chunks, cols, col, k, A, S, h, lds);
     }
     for (int w = 0; w < wave; ++w)
@@ -597,15 +606,17 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; mapD[wave][lane * V + v] = D[v]; }
     __syncthreads();
     if (chunks > 1) {
+        if (wave == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) { A[v] = 1.0f; D[v] = 0.0f; }
+            for (int v = 0; v < V; ++v) { A[v] = 1.0f; D[v] = 0.0f; }
 #pragma unroll
-        for (int w = NW - 1; w >= 0; --w)
+            for (int w = NW - 1; w >= 0; --w)
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                D[v] = apply(mapA[w][lane * V + v], D[v], mapD[w][lane * V + v]);
-                A[v] = compose(A[v], mapA[w][lane * V + v]);
-            }
+                for (int v = 0; v < V; ++v) {
+                    D[v] = apply(mapA[w][lane * V + v], D[v], mapD[w][lane * V + v]);
+                    A[v] = compose(A[v], mapA[w][lane * V + v]);
+                }
+        }
         chain<V, NW>(ws, chunks, cols, col, n, A, D, e, lds);
     }
     for (int w = NW - 1; w > wave; --w)
