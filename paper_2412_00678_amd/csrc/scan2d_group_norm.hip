@@ -468,9 +468,10 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
     if (parts != nullptr) write_parts<V, TH, WAVE>(p, q, l, team, teams, red, accb, accg, parts);
 }
 
-// ---- single rows of up to 64 V channels a group: a group has a power of two of neighbouring lanes (some may be idle), the sums stay in
-// registers and cross the lanes by DPP and lane swaps (through LDS, as above, they took as long as the memory), and the
+// ---- single rows: a group has a power of two of neighbouring lanes (some may be idle), or a wavefront with J times V channels a lane; the
+// sums stay in registers and cross the lanes by DPP and lane swaps (through LDS, as above, they took as long as the memory), and the
 // next items are asked for before these are worked on.
+constexpr int kTokenThreads = 256;
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
 // NR sums over the `lanes` neighbours (a power of two, aligned) of each lane; all of them get them.
@@ -503,70 +504,73 @@ __device__ __forceinline__ void lane_sums(int lanes, float (&s)[NR]) {
         }
     }
 }
-constexpr int kTokenThreads = 256;
 // q.lanes: lanes of a group, a power of two; q.gps, q.slabs: groups of a team, teams of a row.  ONE: V divides a group's channels.
-template <int V, bool ONE>
+template <int V, int J, bool ONE>
 struct TokenLane {
-    int lt, slot, c, lo, width, g;       // first channel, the team's channels, the lane's group
-    bool on, first;                      // has channels; has the group's first
-    bool own[V];
-    bool all;
+    int c[J], mine[J], end, g;           // J times: channel to load from, first own channel; behind the group's last; the group
+    int lo, width;                       // the team's channels
+    bool on, first;                      // has a group; has its first channel
     __device__ TokenLane(const Geo& q, int C, int G, int slab, int lane) {
-        lt = lane;
-        slot = 0;
         const int g0 = slab * q.gps, at = lane / q.lanes, i = lane & (q.lanes - 1);
         lo = g0 * q.D;
         width = min(q.gps, G - g0) * q.D;
-        on = at < q.gps && g0 + at < G && i * V < q.D;
+        on = at < q.gps && g0 + at < G;
         g = min(g0 + at, G - 1);
+        end = (g + 1) * q.D;
         first = on && i == 0;
-        const int mine = g * q.D + i * V;
-        c = min(mine, C - V);
-        all = true;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            own[v] = ONE ? on : on && c + v >= mine && c + v < (g + 1) * q.D;
-            all = all && own[v];
+        for (int j = 0; j < J; ++j) {
+            mine[j] = g * q.D + (j * 64 + i) * V;
+            c[j] = min(mine[j], C - V);
+        }
+    }
+    __device__ __forceinline__ bool any(int j) const { return on && mine[j] < end; }
+    __device__ __forceinline__ bool own(int j, int v) const { return ONE ? any(j) : any(j) && c[j] + v >= mine[j] && c[j] + v < end; }
+    template <typename T>
+    __device__ __forceinline__ void load(const void* x, long long at, Pack<T, V>* to) const {
+#pragma unroll
+        for (int j = 0; j < J; ++j) to[j] = load_pack<T, V>(static_cast<const T*>(x) + at + c[j]);
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(void* to, long long at, int j, const float* v) const {
+        T* const p = static_cast<T*>(to) + at + c[j];
+        if (ONE || (c[j] == mine[j] && mine[j] + V <= end)) {
+            if (any(j)) store_pack<T, V>(p, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (own(j, k)) store_elem(p + k, v[k]);
         }
     }
 };
-// R items' rows of a lane
-template <typename T, int V, int R>
-__device__ __forceinline__ void load_tokens(const GroupNormArgs& p, const void* x, long long sx, int c, long long n0, long long step, Pack<T, V>* to) {
-#pragma unroll
-    for (int i = 0; i < R; ++i) to[i] = load_pack<T, V>(static_cast<const T*>(x) + min(n0 + i * step, (long long)p.N - 1) * sx + c);
-}
-template <typename T, int V, bool ONE>
-__device__ __forceinline__ void store_token(void* to, long long at, const TokenLane<V, ONE>& l, const float* v) {
-    T* const p = static_cast<T*>(to) + at + l.c;
-    if (ONE || l.all) {
-        store_pack<T, V>(p, v);
-    } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (l.own[k]) store_elem(p + k, v[k]);
-    }
-}
-template <typename T, int V, bool ONE, int R, int ACT>
+template <typename T, int V, int J, bool ONE, int R, int ACT>
 __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const GroupNormArgs p, const Geo q, int teams) {
     const int team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts);
-    const TokenLane<V, ONE> l(q, p.C, p.G, team % q.slabs, threadIdx.x & (q.ts - 1));
+    const TokenLane<V, J, ONE> l(q, p.C, p.G, team % q.slabs, threadIdx.x & (q.ts - 1));
     const long long step = teams / q.slabs;
     long long n0 = team < teams ? team / q.slabs : p.N;    // none for lanes to spare
-    Pack<T, V> x[R];
-    load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0, step, x);
-    float gamma[V], beta[V];
-    load_params<V>(p, l.c, gamma, beta);
+    const auto row = [&](long long n) { return min(n, (long long)p.N - 1) * p.sx; };
+    Pack<T, V> x[R][J];
+#pragma unroll
+    for (int i = 0; i < R; ++i) l.template load<T>(p.x, row(n0 + i * step), x[i]);
+    float gamma[J][V], beta[J][V];
+#pragma unroll
+    for (int j = 0; j < J; ++j) load_params<V>(p, l.c[j], gamma[j], beta[j]);
     const float inv = 1.0f / (float)q.D;
     for (long long it = 0; it * R * step < p.N; ++it, n0 += R * step) {
-        Pack<T, V> next[R];
-        if ((it + 1) * R * step < p.N) load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0 + R * step, step, next);
+        Pack<T, V> next[R][J];
+        if ((it + 1) * R * step < p.N) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) l.template load<T>(p.x, row(n0 + (R + i) * step), next[i]);
+        }
         float mean[R], rstd[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             mean[i] = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) mean[i] += l.own[v] ? get<T, V>(x[i], v) : 0.0f;
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) mean[i] += l.own(j, v) ? get<T, V>(x[i][j], v) : 0.0f;
         }
         lane_sums<R>(q.lanes, mean);
 #pragma unroll
@@ -574,10 +578,12 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const 
             mean[i] *= inv;
             rstd[i] = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float d = l.own[v] ? get<T, V>(x[i], v) - mean[i] : 0.0f;
-                rstd[i] = fmaf(d, d, rstd[i]);
-            }
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float d = l.own(j, v) ? get<T, V>(x[i][j], v) - mean[i] : 0.0f;
+                    rstd[i] = fmaf(d, d, rstd[i]);
+                }
         }
         lane_sums<R>(q.lanes, rstd);
 #pragma unroll
@@ -586,54 +592,65 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_kernel(const 
             if (n < p.N && l.on) {
                 const bool out = p.mask != nullptr && p.mask[n] != 0;
                 const float m = out ? 0.0f : mean[i], rs = out ? 0.0f : 1.0f / sqrtf(rstd[i] * inv + p.eps);
-                float y[V];
 #pragma unroll
-                for (int v = 0; v < V; ++v) y[v] = out ? 0.0f : act_of<ACT>(fmaf((get<T, V>(x[i], v) - m) * rs, gamma[v], beta[v]));
-                store_token<T, V, ONE>(p.y, n * p.sy, l, y);
+                for (int j = 0; j < J; ++j) {
+                    float y[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) y[v] = out ? 0.0f : act_of<ACT>(fmaf((get<T, V>(x[i][j], v) - m) * rs, gamma[j][v], beta[j][v]));
+                    l.template store<T>(p.y, n * p.sy, j, y);
+                }
                 if (l.first) {
                     float* st = p.stats + ((size_t)n * p.G + l.g) * 2;
                     st[0] = m;
                     st[1] = rs;
                 }
             }
-            x[i] = next[i];
+#pragma unroll
+            for (int j = 0; j < J; ++j) x[i][j] = next[i][j];
         }
     }
 }
-template <typename T, int V, bool ONE, int R, int ACT>
+template <typename T, int V, int J, bool ONE, int R, int ACT>
 __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(const GroupNormArgs p, const Geo q, int teams, float2* parts) {
-    __shared__ float red[2 * kTokenThreads * V];
-    const int team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts);
-    const TokenLane<V, ONE> l(q, p.C, p.G, team % q.slabs, threadIdx.x & (q.ts - 1));
+    constexpr bool AHEAD = J == 1;                          // several times V channels: no registers left for the next items
+    __shared__ float red[2 * kTokenThreads * V * J];
+    const int lt = threadIdx.x & (q.ts - 1), team = (int)((blockIdx.x * (long long)kTokenThreads + threadIdx.x) / q.ts);
+    const TokenLane<V, J, ONE> l(q, p.C, p.G, team % q.slabs, lt);
     const long long step = teams / q.slabs;
     long long n0 = team < teams ? team / q.slabs : p.N;
-    Pack<T, V> x[R], dy[R];
-    float mean[R], rstd[R];
-    const auto load_stats = [&](long long from, float* m, float* r) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const float* st = p.stats + ((size_t)min(from + i * step, (long long)p.N - 1) * p.G + l.g) * 2;
-            m[i] = st[0];
-            r[i] = st[1];
-        }
+    struct Item {
+        Pack<T, V> x[J], dy[J];
+        float mean, rstd;
     };
-    load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0, step, x);
-    load_tokens<T, V, R>(p, p.dy, p.sdy, l.c, n0, step, dy);
-    load_stats(n0, mean, rstd);
-    float gamma[V], beta[V], accb[V], accg[V];
-    load_params<V>(p, l.c, gamma, beta);
+    const auto load = [&](long long n, Item& to) {
+        n = min(n, (long long)p.N - 1);
+        l.template load<T>(p.x, n * p.sx, to.x);
+        l.template load<T>(p.dy, n * p.sdy, to.dy);
+        const float* st = p.stats + ((size_t)n * p.G + l.g) * 2;
+        to.mean = st[0];
+        to.rstd = st[1];
+    };
+    Item w[R];
+    if (AHEAD) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) accb[v] = accg[v] = 0.0f;
+        for (int i = 0; i < R; ++i) load(n0 + i * step, w[i]);
+    }
+    float gamma[J][V], beta[J][V], accb[J][V], accg[J][V];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        load_params<V>(p, l.c[j], gamma[j], beta[j]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) accb[j][v] = accg[j][v] = 0.0f;
+    }
     const float inv = 1.0f / (float)q.D;
     for (long long it = 0; it * R * step < p.N; ++it, n0 += R * step) {
-        Pack<T, V> nx[R], ndy[R];
-        float nmean[R], nrstd[R];
-        if ((it + 1) * R * step < p.N) {
-            load_tokens<T, V, R>(p, p.x, p.sx, l.c, n0 + R * step, step, nx);
-            load_tokens<T, V, R>(p, p.dy, p.sdy, l.c, n0 + R * step, step, ndy);
-            load_stats(n0 + R * step, nmean, nrstd);
+        Item next[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (!AHEAD) load(n0 + i * step, w[i]);
+            else if ((it + 1) * R * step < p.N) load(n0 + (R + i) * step, next[i]);
         }
-        float s1[R], s2[R], dv[R][V];
+        float s1[R], s2[R], dv[R][J][V];
         bool live[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -641,16 +658,18 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(co
             live[i] = n < p.N && l.on && (p.mask == nullptr || p.mask[n] == 0);
             s1[i] = s2[i] = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const bool counts = ONE ? live[i] : live[i] && l.own[v];
-                const float xh = (get<T, V>(x[i], v) - mean[i]) * rstd[i];
-                dv[i][v] = counts ? get<T, V>(dy[i], v) * act_slope<ACT>(fmaf(xh, gamma[v], beta[v])) : 0.0f;
-                const float g = counts ? dv[i][v] * xh : 0.0f;
-                accb[v] += dv[i][v];
-                accg[v] += g;
-                s1[i] = fmaf(dv[i][v], gamma[v], s1[i]);
-                s2[i] = fmaf(g, gamma[v], s2[i]);
-            }
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const bool counts = live[i] && l.own(j, v);
+                    const float xh = (get<T, V>(w[i].x[j], v) - w[i].mean) * w[i].rstd;
+                    dv[i][j][v] = counts ? get<T, V>(w[i].dy[j], v) * act_slope<ACT>(fmaf(xh, gamma[j][v], beta[j][v])) : 0.0f;
+                    const float g = counts ? dv[i][j][v] * xh : 0.0f;
+                    accb[j][v] += dv[i][j][v];
+                    accg[j][v] += g;
+                    s1[i] = fmaf(dv[i][j][v], gamma[j][v], s1[i]);
+                    s2[i] = fmaf(g, gamma[j][v], s2[i]);
+                }
         }
         lane_sums<R>(q.lanes, s1);
         lane_sums<R>(q.lanes, s2);
@@ -658,18 +677,41 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(co
         for (int i = 0; i < R; ++i) {
             const long long n = n0 + i * step;
             if (n < p.N && l.on) {
-                float dx[V];
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float xh = (get<T, V>(x[i], v) - mean[i]) * rstd[i];
-                    dx[v] = live[i] ? rstd[i] * (fmaf(dv[i][v], gamma[v], -s1[i] * inv) - xh * (s2[i] * inv)) : 0.0f;
+                for (int j = 0; j < J; ++j) {
+                    float dx[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const float xh = (get<T, V>(w[i].x[j], v) - w[i].mean) * w[i].rstd;
+                        dx[v] = live[i] ? w[i].rstd * (fmaf(dv[i][j][v], gamma[j][v], -s1[i] * inv) - xh * (s2[i] * inv)) : 0.0f;
+                    }
+                    l.template store<T>(p.dx, n * p.sdx, j, dx);
                 }
-                store_token<T, V, ONE>(p.dx, n * p.sdx, l, dx);
             }
-            x[i] = nx[i]; dy[i] = ndy[i]; mean[i] = nmean[i]; rstd[i] = nrstd[i];
+            if (AHEAD) w[i] = next[i];
         }
     }
-    if (parts != nullptr) write_parts<V, kTokenThreads, true>(p, q, l, team, teams, red, accb, accg, parts);
+    if (parts == nullptr) return;
+    // where a row is one team's, the sums of all the workgroup's teams together
+    const bool together = q.slabs == 1;
+    const int teams_here = together ? kTokenThreads / q.ts : 1, size = teams_here * q.ts * V * J, at = together ? (int)threadIdx.x / q.ts : 0;
+    float* const sums = together ? red : red + 2 * (threadIdx.x - lt) * V * J;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (l.own(j, v)) {
+                sums[at * l.width + l.c[j] + v - l.lo] = accb[j][v];
+                sums[size + at * l.width + l.c[j] + v - l.lo] = accg[j][v];
+            }
+    __syncthreads();
+    if (team >= teams && !together) return;
+    float2* const to = parts + (size_t)(together ? (int)blockIdx.x : team / q.slabs) * p.C + l.lo;
+    for (int c = together ? threadIdx.x : lt; c < l.width; c += together ? kTokenThreads : q.ts) {
+        float b = 0.0f, g = 0.0f;
+        for (int k = 0; k < teams_here; ++k) { b += sums[k * l.width + c]; g += sums[size + k * l.width + c]; }
+        to[c] = make_float2(b, g);
+    }
 }
 
 // dbeta and dgamma from E parts of them: 16 channels x 64 shares of the parts per workgroup, joined in order.
@@ -910,65 +952,96 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
     if (t.slab == 0 && threadIdx.x == 0) counts[(size_t)t.n * chunks + t.chunk] = (float)rows;
 }
 
-// Joins the tiles' sums of an item, for some of its groups per workgroup (at least 16 channels, 128 bytes a row): chan[n][C], and
-// coef[n][G] = (sum dv gamma, sum dv gamma xh) / M.  Where there is only one item, its sums are dbeta and dgamma.
-constexpr int kJoinThreads = 1024;
+// Joins the tiles' sums of an item, for `gw` of its groups per workgroup (up to kNarrow channels a group, at least 16 channels, 128 bytes
+// a row, together): chan[n][C], and coef[n][G] = (sum dv gamma, sum dv gamma xh) / M.  Where there is only one item, its sums are dbeta and dgamma.
+constexpr int kJoinThreads = 1024, kNarrow = 64;
+__device__ __forceinline__ float block_rows(const float* counts, size_t n, int chunks, float* rows_of) {
+    float rows = 0.0f;
+    for (int k = threadIdx.x; k < chunks; k += kJoinThreads) rows += counts[n * chunks + k];
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) rows += __shfl_xor(rows, m);
+    if ((threadIdx.x & 63) == 0) rows_of[threadIdx.x >> 6] = rows;
+    __syncthreads();
+    rows = 0.0f;
+    for (int k = 0; k < kJoinThreads / 64; ++k) rows += rows_of[k];
+    return rows;
+}
 __global__ __launch_bounds__(kJoinThreads) void group_norm_chan_kernel(const float2* sums, const float* counts, int chunks, int C, int G, int D, int gw,
                                                                        const float* gamma, float2* chan, float2* coef, float* dgamma, float* dbeta) {
     __shared__ float2 red[kJoinThreads], total[kJoinThreads];
     __shared__ float rows_of[kJoinThreads / 64];
     const int tid = threadIdx.x, sets = (G + gw - 1) / gw, g0 = (blockIdx.x % sets) * gw;
     const size_t n = blockIdx.x / sets;
-    const int groups = min(gw, G - g0), width = groups * D, lo = g0 * D;
-    float rows = 0.0f;
-    for (int k = tid; k < chunks; k += kJoinThreads) rows += counts[n * chunks + k];
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) rows += __shfl_xor(rows, m);
-    if ((tid & 63) == 0) rows_of[tid >> 6] = rows;
-    float2 mine = make_float2(0.0f, 0.0f);                  // of a group's gamma-weighted sums, in the lanes that keep them
-    for (int c0 = 0; c0 < width; c0 += kJoinThreads) {      // more than one turn only for a group of more channels than threads
-        const int w = min(width - c0, kJoinThreads), shares = kJoinThreads / w, c = tid % w, share = tid / w;
-        float2 s = make_float2(0.0f, 0.0f);
-        if (share < shares) {
+    const int groups = min(gw, G - g0), w = groups * D, lo = g0 * D, shares = kJoinThreads / w, c = tid % w, share = tid / w;
+    float2 s = make_float2(0.0f, 0.0f);
+    if (share < shares) {
 #pragma unroll 8
-            for (int k = share; k < chunks; k += shares) {
-                const float2 t = sums[(n * chunks + k) * C + lo + c0 + c];
-                s.x += t.x; s.y += t.y;
-            }
-        }
-        __syncthreads();
-        red[tid] = s;
-        __syncthreads();
-        if (tid < w) {
-            for (int k = 1; k < shares; ++k) { s.x += red[k * w + c].x; s.y += red[k * w + c].y; }
-            const int ch = lo + c0 + c;
-            if (chan) chan[n * C + ch] = s;
-            if (dbeta) dbeta[ch] = s.x;
-            if (dgamma) dgamma[ch] = s.y;
-            const float gm = gamma ? gamma[ch] : 1.0f;
-            total[tid] = make_float2(s.x * gm, s.y * gm);
-        }
-        __syncthreads();
-        if (groups == 1) {                                  // all threads on one group
-            if (tid < w) { mine.x += total[tid].x; mine.y += total[tid].y; }
-        } else if (tid < groups) {
-            for (int d = 0; d < D; ++d) { mine.x += total[tid * D + d].x; mine.y += total[tid * D + d].y; }
+        for (int k = share; k < chunks; k += shares) {
+            const float2 t = sums[(n * chunks + k) * C + lo + c];
+            s.x += t.x; s.y += t.y;
         }
     }
-    if (groups == 1) {
-        __syncthreads();
-        total[tid] = mine;
-        for (int m = kJoinThreads / 2; m > 0; m >>= 1) {
-            __syncthreads();
-            if (tid < m) { total[tid].x += total[tid + m].x; total[tid].y += total[tid + m].y; }
-        }
-        mine = total[0];
+    red[tid] = s;
+    const float rows = block_rows(counts, n, chunks, rows_of);          // behind its barrier red is there
+    if (tid < w) {
+        for (int k = 1; k < shares; ++k) { s.x += red[k * w + c].x; s.y += red[k * w + c].y; }
+        if (chan) chan[n * C + lo + c] = s;
+        if (dbeta) dbeta[lo + c] = s.x;
+        if (dgamma) dgamma[lo + c] = s.y;
+        const float gm = gamma ? gamma[lo + c] : 1.0f;
+        total[tid] = make_float2(s.x * gm, s.y * gm);
     }
+    __syncthreads();
     if (tid < groups) {
-        float M = 0.0f;
-        for (int k = 0; k < kJoinThreads / 64; ++k) M += rows_of[k];
-        const float inv = M > 0.0f ? 1.0f / (M * (float)D) : 0.0f;
-        coef[n * G + g0 + tid] = make_float2(mine.x * inv, mine.y * inv);
+        const float inv = rows > 0.0f ? 1.0f / (rows * (float)D) : 0.0f;
+        float2 t = make_float2(0.0f, 0.0f);
+        for (int d = 0; d < D; ++d) { t.x += total[tid * D + d].x; t.y += total[tid * D + d].y; }
+        coef[n * G + g0 + tid] = make_float2(t.x * inv, t.y * inv);
+    }
+}
+// Wider groups: 16 channels of an item per workgroup, then one workgroup per item and group.
+__global__ __launch_bounds__(kJoinThreads) void group_norm_wide_chan_kernel(const float2* sums, int chunks, int C, float2* chan, float* dgamma, float* dbeta) {
+    __shared__ float2 red[64][16];
+    const int cols = (C + 15) / 16, lane = threadIdx.x & 15, share = threadIdx.x >> 4, c = (blockIdx.x % cols) * 16 + lane;
+    const size_t n = blockIdx.x / cols;
+    float2 s = make_float2(0.0f, 0.0f);
+    if (c < C) {
+#pragma unroll 8
+        for (int k = share; k < chunks; k += 64) {
+            const float2 t = sums[(n * chunks + k) * C + c];
+            s.x += t.x; s.y += t.y;
+        }
+    }
+    red[share][lane] = s;
+    __syncthreads();
+    if (share == 0 && c < C) {
+        for (int k = 1; k < 64; ++k) { s.x += red[k][lane].x; s.y += red[k][lane].y; }
+        chan[n * C + c] = s;
+        if (dbeta) dbeta[c] = s.x;
+        if (dgamma) dgamma[c] = s.y;
+    }
+}
+__global__ __launch_bounds__(kJoinThreads) void group_norm_wide_coef_kernel(const float2* chan, const float* counts, int chunks, int G, int D, const float* gamma,
+                                                                            float2* coef) {
+    __shared__ float2 red[kJoinThreads / 64];
+    __shared__ float rows_of[kJoinThreads / 64];
+    const int tid = threadIdx.x, g = blockIdx.x % G;
+    const size_t n = blockIdx.x / G;
+    float2 t = make_float2(0.0f, 0.0f);
+    for (int d = tid; d < D; d += kJoinThreads) {
+        const float2 c = chan[(n * G + g) * D + d];
+        const float gm = gamma ? gamma[(size_t)g * D + d] : 1.0f;
+        t.x = fmaf(c.x, gm, t.x);
+        t.y = fmaf(c.y, gm, t.y);
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) { t.x += __shfl_xor(t.x, m); t.y += __shfl_xor(t.y, m); }
+    if ((tid & 63) == 0) red[tid >> 6] = t;
+    const float rows = block_rows(counts, n, chunks, rows_of);
+    if (tid == 0) {
+        const float inv = rows > 0.0f ? 1.0f / (rows * (float)D) : 0.0f;
+        for (int k = 1; k < kJoinThreads / 64; ++k) { t.x += red[k].x; t.y += red[k].y; }
+        coef[n * G + g] = make_float2(t.x * inv, t.y * inv);
     }
 }
 
@@ -1030,6 +1103,7 @@ constexpr int kTileWgs = 512;            // tiles of the split form, at least, w
 enum { FORM_WAVE = 0, FORM_GROUP = 1, FORM_SPLIT = 2, FORM_TOKENS = 3 };
 constexpr int kHeldRows = 8, kWaveThreads = 256, kGroupThreads = 512;
 constexpr int kItems = 4, kItemsBwd = 2;                   // single rows that a lane takes at once
+constexpr int kTokenChannels = 2048;                       // of a group, at most: 32 a lane
 constexpr int kTokenWgs = 1024;                            // four workgroups of single rows per compute unit
 
 int floor_pow2(int v) {
@@ -1089,7 +1163,7 @@ NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
     };
     // single rows: the widest loads, and as many groups to a wavefront as it has lanes for
     const int TV = d->dtype == SCAN2D_BF16 && D >= 8 ? 8 : 4;
-    if (d->P == 1 && d->C >= 4 && D <= 64 * TV) {
+    if (d->P == 1 && d->C >= 4 && D <= kTokenChannels) {
         n.form = FORM_TOKENS;
         n.V = TV;
         n.K = 1;
@@ -1097,7 +1171,7 @@ NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
         n.q = Geo();
         n.q.D = D;
         n.q.lanes = 1;
-        while (n.q.lanes * TV < D) n.q.lanes *= 2;
+        while (n.q.lanes < 64 && n.q.lanes * TV < D) n.q.lanes *= 2;
         n.q.ts = n.q.lanes;
         while (n.q.ts < 64 && n.q.ts / n.q.lanes < d->G) n.q.ts *= 2;
         n.q.gps = n.q.ts / n.q.lanes;
@@ -1127,7 +1201,12 @@ NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
         if ((long long)n.q.slots * kHeldRows >= d->P) return held(FORM_GROUP, kMaxWgs);
     }
     n.form = FORM_SPLIT;
+    // whole rows, or narrower slabs where they keep more lanes busy (1192 channels in two groups: 298 of 512, 447 with a group a slab)
     (void)fill_geo(d, n.V, kTileThreads, kTileThreads * n.V, false, &n.q);
+    for (int most = kTileThreads * n.V / 2; most >= 128; most /= 2) {
+        Geo q;
+        if (fill_geo(d, n.V, kTileThreads, most, false, &q) && q.slots * q.width * 10 > n.q.slots * n.q.width * 11) n.q = q;
+    }
     const long long batch = (long long)n.q.slots * kRows, batches = (d->P + batch - 1) / batch, each = (long long)d->N * n.q.slabs;
     long long chunks = (kTileWgs + each - 1) / each;
     if (chunks > batches) chunks = batches;
@@ -1191,9 +1270,10 @@ template <typename T, int V, bool ONE, int ACT>
 int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
     const unsigned cols = (a.C + 15) / 16;
+    const bool narrow = a.D <= kNarrow;
     const int gw = a.D >= 16 ? 1 : (16 + a.D - 1) / a.D, sets = (a.G + gw - 1) / gw;
-    const long long blocks = (long long)a.N * n.chunks * n.q.slabs, joins = (long long)a.N * sets;
-    if (!launch_fits(blocks + cols, kTileThreads) || !launch_fits(joins, kJoinThreads)) return SCAN2D_ERR_BAD_SHAPE;
+    const long long blocks = (long long)a.N * n.chunks * n.q.slabs, joins = (long long)a.N * (narrow ? sets : cols), groups = (long long)a.N * a.G;
+    if (!launch_fits(blocks + cols, kTileThreads) || !launch_fits(joins, kJoinThreads) || !launch_fits(groups, kJoinThreads)) return SCAN2D_ERR_BAD_SHAPE;
     char* w = static_cast<char*>(a.workspace);
     const size_t items = (size_t)a.N * n.chunks;
     float2* sums = reinterpret_cast<float2*>(w);
@@ -1205,48 +1285,59 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     float2* coef = reinterpret_cast<float2*>(w);
     const bool several = params && a.N > 1;
     hipLaunchKernelGGL((group_norm_sums_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, sums, counts);
-    hipLaunchKernelGGL(group_norm_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, a.C, a.G, a.D, gw, a.gamma,
-                       several ? chan : nullptr, coef, several ? nullptr : a.dgamma, several ? nullptr : a.dbeta);
+    float *const dgamma = several ? nullptr : a.dgamma, *const dbeta = several ? nullptr : a.dbeta;
+    if (narrow) {
+        hipLaunchKernelGGL(group_norm_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, a.C, a.G, a.D, gw, a.gamma,
+                           several ? chan : nullptr, coef, dgamma, dbeta);
+    } else {
+        hipLaunchKernelGGL(group_norm_wide_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, n.chunks, a.C, chan, dgamma, dbeta);
+        hipLaunchKernelGGL(group_norm_wide_coef_kernel, dim3((unsigned)groups), dim3(kJoinThreads), 0, stream, chan, counts, n.chunks, a.G, a.D, a.gamma, coef);
+    }
     hipLaunchKernelGGL((group_norm_grad_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks + (several ? cols : 0)), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, coef,
                        (unsigned)blocks, chan);
     return launched();
 }
 
-template <typename T, int V, bool ONE, int ACT>
-int fwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
-    if (n.form == FORM_TOKENS) {
-        if constexpr (V > 1) {
-            const long long blocks = (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads;
-            hipLaunchKernelGGL((group_norm_tokens_kernel<T, V, ONE, 16 / V, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams);
-        }
+// single rows: J times V channels a lane
+template <typename T, int V, int J, bool ONE, int ACT>
+int tokens(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
+    const dim3 blocks((unsigned)((n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads));
+    if (!backward) {
+        hipLaunchKernelGGL((group_norm_tokens_kernel<T, V, J, ONE, J == 1 ? 16 / V : 1, ACT>), blocks, dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams);
         return launched();
     }
-    if constexpr (V <= 4) return n.form == FORM_SPLIT ? fwd_split<T, V, ONE, ACT>(a, n, stream) : fwd_held<T, V, ONE, ACT>(a, n, stream);
-    return SCAN2D_ERR_BAD_SHAPE;                            // eight channels of a lane: single rows only
+    const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
+    float2* parts = params ? static_cast<float2*>(a.workspace) : nullptr;
+    hipLaunchKernelGGL((group_norm_tokens_bwd_kernel<T, V, J, ONE, J == 1 && V == 4 ? 2 : 1, ACT>), blocks, dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams, parts);
+    if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3((a.C + 15) / 16), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
+    return launched();
 }
 template <typename T, int V, bool ONE, int ACT>
-int bwd(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
-    const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
-    const unsigned cols = (a.C + 15) / 16;
+int run(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
     if (n.form == FORM_TOKENS) {
         if constexpr (V > 1) {
-            const long long blocks = (n.teams * n.q.ts + kTokenThreads - 1) / kTokenThreads;
-            float2* parts = params ? static_cast<float2*>(a.workspace) : nullptr;
-            hipLaunchKernelGGL((group_norm_tokens_bwd_kernel<T, V, ONE, V == 8 ? 1 : 2, ACT>), dim3((unsigned)blocks), dim3(kTokenThreads), 0, stream, a, n.q, (int)n.teams, parts);
-            if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3(cols), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
+            const int times = (a.D + 64 * V - 1) / (64 * V);
+            if (times == 1) return tokens<T, V, 1, ONE, ACT>(a, n, backward, stream);
+            if constexpr (V * Elem<T>::kBytes == 16) {      // 16 bytes a load
+                if (times == 2) return tokens<T, V, 2, ONE, ACT>(a, n, backward, stream);
+                if (times <= 4) return tokens<T, V, 4, ONE, ACT>(a, n, backward, stream);
+                if constexpr (V == 4) return tokens<T, V, 8, ONE, ACT>(a, n, backward, stream);
+            }
         }
-        return launched();
+    } else if constexpr (V <= 4) {                          // eight channels of a lane: single rows only
+        if (backward) return n.form == FORM_SPLIT ? bwd_split<T, V, ONE, ACT>(a, n, stream) : bwd_held<T, V, ONE, ACT>(a, n, stream);
+        return n.form == FORM_SPLIT ? fwd_split<T, V, ONE, ACT>(a, n, stream) : fwd_held<T, V, ONE, ACT>(a, n, stream);
     }
-    if constexpr (V <= 4) return n.form == FORM_SPLIT ? bwd_split<T, V, ONE, ACT>(a, n, stream) : bwd_held<T, V, ONE, ACT>(a, n, stream);
     return SCAN2D_ERR_BAD_SHAPE;
 }
+
 template <typename T, int V, bool ONE>
 int by_act(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t stream) {
     (void)hipGetLastError();
     switch (a.act) {
-        case SCAN2D_ACT_SILU: return backward ? bwd<T, V, ONE, SCAN2D_ACT_SILU>(a, n, stream) : fwd<T, V, ONE, SCAN2D_ACT_SILU>(a, n, stream);
-        case SCAN2D_ACT_GELU: return backward ? bwd<T, V, ONE, SCAN2D_ACT_GELU>(a, n, stream) : fwd<T, V, ONE, SCAN2D_ACT_GELU>(a, n, stream);
-        default: return backward ? bwd<T, V, ONE, SCAN2D_ACT_NONE>(a, n, stream) : fwd<T, V, ONE, SCAN2D_ACT_NONE>(a, n, stream);
+        case SCAN2D_ACT_SILU: return run<T, V, ONE, SCAN2D_ACT_SILU>(a, n, backward, stream);
+        case SCAN2D_ACT_GELU: return run<T, V, ONE, SCAN2D_ACT_GELU>(a, n, backward, stream);
+        default: return run<T, V, ONE, SCAN2D_ACT_NONE>(a, n, backward, stream);
     }
 }
 template <typename T>

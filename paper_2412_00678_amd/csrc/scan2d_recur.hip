@@ -160,22 +160,41 @@ __device__ __forceinline__ RowBits row_bits(const RecurArgs& p, const SeqSearch&
     r.first = r.last = 0;
     r.inside = ~0ull;
     if (!r.plain) {
-        int s = s0;
+        int s = s0;                                         // this lane's row's sequence, and its rows
+        Span w = {lo, hi};
         if (p.offsets) {
-            while (lane < TW && s < p.S && p.offsets[s + 1] <= t) ++s;     // past the ends between t0 and this row
+            // 64 ends at a time from the first row's on, in the lanes; the rows' lanes go past them one after the other
+            for (int base = p.S <= 64 ? 0 : s0; base < p.S; base += 64) {
+                const int end = p.S <= 64 ? search.end : base + lane < p.S ? p.offsets[base + lane + 1] : 0x7fffffff;
+                const int last = min(p.S - base, 64);
+                int k = max(s0 - base, 0);
+                for (; k < last; ++k) {
+                    const int e = __builtin_amdgcn_readlane(end, k);
+                    if (e >= t0 + TW) break;                // it ends behind the last row
+                    if (t >= e) {
+                        s = base + k + 1;
+                        w.lo = e;
+                        w.hi = -1;                          // known once the next end is
+                    } else if (s == base + k) {
+                        w.hi = e;
+                    }
+                }
+                if (k < last) {
+                    const int e = __builtin_amdgcn_readlane(end, k);
+                    if (s == base + k) w.hi = e;
+                    break;
+                }
+            }
+            w.lo = max(w.lo, 0);
+            w.hi = min(w.hi, p.T);
         } else if (p.per > 0) {
             s = t / p.per;
+            if (s < p.S) w = span_of(p, s);
         }
-        bool first = false, last = false, inside = false;
-        if (lane < TW && t < p.T && s < p.S) {
-            const Span w = span_of(p, s);
-            inside = t >= w.lo && t < w.hi;
-            first = inside && t == w.lo;
-            last = inside && t + 1 == w.hi;
-        }
+        const bool inside = lane < TW && t < p.T && s < p.S && t >= w.lo && t < w.hi;
         r.seq = s;
-        r.first = __ballot(first);
-        r.last = __ballot(last);
+        r.first = __ballot(inside && t == w.lo);
+        r.last = __ballot(inside && t + 1 == w.hi);
         r.inside = __ballot(inside);
     }
     return r;
@@ -370,14 +389,48 @@ __device__ __forceinline__ Gates gates(const Pack<T, V>& r, const Pack<T, V>& i,
     return g;
 }
 __device__ __forceinline__ bool bit(uint64_t m, int j) { return ((m >> j) & 1) != 0; }
+// The values that the first two of the marked rows read of an [S][C] array (h0 at first rows, dhT at last ones), asked for
+// together and ahead; those of further rows, in wavefronts of sequences of a few rows, one by one.
+template <int V>
+struct Ahead {
+    const float* from;
+    int row0, row1;
+    float val0[V], val1[V];
+    __device__ __forceinline__ Ahead(const RecurArgs& p, const RowBits& bits, uint64_t marked, const float* array, int c) : from(array) {
+        const uint64_t behind = marked & (marked - 1);
+        row0 = array != nullptr && marked != 0 ? __builtin_ctzll(marked) : -1;
+        row1 = array != nullptr && behind != 0 ? __builtin_ctzll(behind) : -1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) val0[v] = val1[v] = 0.0f;
+        if (row0 >= 0) {
+            const float* q = from + (size_t)bits.seq_of(row0) * p.C + c;
+#pragma unroll
+            for (int v = 0; v < V; ++v) val0[v] = q[v];
+        }
+        if (row1 >= 0) {
+            const float* q = from + (size_t)bits.seq_of(row1) * p.C + c;
+#pragma unroll
+            for (int v = 0; v < V; ++v) val1[v] = q[v];
+        }
+    }
+    __device__ __forceinline__ float get(const RecurArgs& p, const RowBits& bits, int j, int c, int v) const {
+        if (j != row0 && j != row1) return from[(size_t)bits.seq_of(j) * p.C + c + v];
+        float a = val0[v], b = val1[v];
+        asm("" : "+v"(a), "+v"(b));                         // values, not the places they are in: those would be in scratch memory
+        return j == row0 ? a : b;
+    }
+};
 // a row's map on top of (A, S); `plain`: known to be neither a first row nor one of no sequence
 template <bool PLAIN, int V>
-__device__ __forceinline__ void add_row(const RecurArgs& p, const RowBits& bits, int j, int c, const float* a, float* u, float* A, float* S) {
+__device__ __forceinline__ void add_row(const RecurArgs& p, const RowBits& bits, int j, int c, const float* a, float* u, float* A, float* S,
+                                        const Ahead<V> h0) {
     if (!PLAIN && bit(bits.first, j)) {
-        const float* h0 = p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+        if (p.h0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) u[v] = fmaf(a[v], h0.get(p, bits, j, c, v), u[v]);
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (h0) u[v] = fmaf(a[v], h0[v], u[v]);
             S[v] = u[v];
             A[v] = kCut;
         }
@@ -395,12 +448,13 @@ __device__ __forceinline__ void add_row(const RecurArgs& p, const RowBits& bits,
 
 // ---- forward
 template <int V, int TW, bool PLAIN>
-__device__ __forceinline__ void add_rows(const RecurArgs& p, const RowBits& bits, int c, const float (*a)[V], float (*u)[V], float* A, float* S) {
+__device__ __forceinline__ void add_rows(const RecurArgs& p, const RowBits& bits, int c, const float (*a)[V], float (*u)[V], float* A, float* S,
+                                         const Ahead<V> h0) {
 #pragma unroll
-    for (int j = 0; j < TW; ++j) add_row<PLAIN, V>(p, bits, j, c, a[j], u[j], A, S);
+    for (int j = 0; j < TW; ++j) add_row<PLAIN, V>(p, bits, j, c, a[j], u[j], A, S, h0);
 }
 template <typename T, int V, int TW, bool PLAIN>
-__device__ __forceinline__ void fwd_rows(const RecurArgs& p, const RowBits& bits, int c, uint32_t off, const RowPointer& row, const float (*a)[V],
+__device__ __forceinline__ void fwd_rows(const RecurArgs& p, const RowBits& bits, int c, uint32_t off, const RowPointer row, const float (*a)[V],
                                          const float (*u)[V], float* h) {
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
@@ -439,6 +493,7 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
             ir[j] = load_pack<T, V>(pi.at, off + pi.row_or_last(j));
         }
     }
+    const Ahead<V> h0(p, bits, bits.first, p.h0, c);
     float decay[V], A[V], S[V], h[V], a[TW][V], u[TW][V];
 #pragma unroll
     for (int v = 0; v < V; ++v) { decay[v] = lds.decay[lane * V + v]; A[v] = 1.0f; S[v] = h[v] = 0.0f; }
@@ -450,8 +505,8 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
             a[j][v] = g.a;
             u[j][v] = g.b * g.si * get<T, V>(xr[j], v);
         }
-    if (bits.plain) add_rows<V, TW, true>(p, bits, c, a, u, A, S);
-    else add_rows<V, TW, false>(p, bits, c, a, u, A, S);
+    if (bits.plain) add_rows<V, TW, true>(p, bits, c, a, u, A, S, h0);
+    else add_rows<V, TW, false>(p, bits, c, a, u, A, S, h0);
 #pragma unroll
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; }
     __syncthreads();
@@ -488,8 +543,9 @@ struct BwdRows {
     float a[TW][V], u[TW][V], sr[TW][V], si[TW][V], b[TW][V];
 };
 template <typename T, int V, int TW, bool PLAIN>
-__device__ __forceinline__ void bwd_maps(const RecurArgs& p, const RowBits& bits, int c, BwdRows<T, V, TW>& w, float* A, float* S, float* D) {
-    add_rows<V, TW, PLAIN>(p, bits, c, w.a, w.u, A, S);
+__device__ __forceinline__ void bwd_maps(const RecurArgs& p, const RowBits& bits, int c, BwdRows<T, V, TW>& w, float* A, float* S, float* D,
+                                         const Ahead<V> h0, const Ahead<V> dhT) {
+    add_rows<V, TW, PLAIN>(p, bits, c, w.a, w.u, A, S, h0);
     // e in front of the rows from the one behind them: D + A e.  Behind a sequence's last row there is another's first, whose e
     // does not come here, or a row of none: D is 0 there.
 #pragma unroll
@@ -498,23 +554,23 @@ __device__ __forceinline__ void bwd_maps(const RecurArgs& p, const RowBits& bits
 #pragma unroll
             for (int v = 0; v < V; ++v) D[v] = 0.0f;
         } else {
-            const float* dT = !PLAIN && p.dhT && bit(bits.last, j) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+            const bool last = !PLAIN && p.dhT && bit(bits.last, j);
 #pragma unroll
-            for (int v = 0; v < V; ++v) D[v] = w.a[j][v] * (get<T, V>(w.dh[j], v) + D[v] + (dT ? dT[v] : 0.0f));
+            for (int v = 0; v < V; ++v) D[v] = w.a[j][v] * (get<T, V>(w.dh[j], v) + D[v] + (last ? dhT.get(p, bits, j, c, v) : 0.0f));
         }
     }
 }
 template <typename T, int V, int TW, bool PLAIN>
 __device__ __forceinline__ void bwd_rows(const RecurArgs& p, const RowBits& bits, int t0, int c, uint32_t off, const float* decay, BwdRows<T, V, TW>& w,
-                                         float* h, float* e, float* sum) {
+                                         float* h, float* e, float* sum, const Ahead<V> h0, const Ahead<V> dhT) {
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
         const bool first = !PLAIN && bit(bits.first, j), cut = first || (!PLAIN && !bit(bits.inside, j));
-        const float* h0 = first && p.h0 ? p.h0 + (size_t)bits.seq_of(j) * p.C + c : nullptr;
+        const bool start = first && p.h0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float next = cut ? w.u[j][v] : fmaf(w.a[j][v], h[v], w.u[j][v]);
-            w.u[j][v] = cut ? (h0 ? h0[v] : 0.0f) : h[v];
+            w.u[j][v] = cut ? (start ? h0.get(p, bits, j, c, v) : 0.0f) : h[v];
             h[v] = next;
         }
     }
@@ -526,13 +582,13 @@ __device__ __forceinline__ void bwd_rows(const RecurArgs& p, const RowBits& bits
 #pragma unroll
     for (int j = TW - 1; j >= 0; --j) {
         if (PLAIN || bit(bits.inside, j)) {
-            const float* dT = !PLAIN && p.dhT && bit(bits.last, j) ? p.dhT + (size_t)bits.seq_of(j) * p.C + c : nullptr;
             float dx[V], di[V], dr[V];
+            const bool last = !PLAIN && p.dhT && bit(bits.last, j);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float a = w.a[j][v], b = w.b[j][v], si = w.si[j][v], sr = w.sr[j][v], x = get<T, V>(w.x[j], v);
                 const float ib = b > 0.0f ? __builtin_amdgcn_rcpf(b) : 0.0f;
-                const float g = get<T, V>(w.dh[j], v) + e[v] + (dT ? dT[v] : 0.0f), gs = g * si;
+                const float g = get<T, V>(w.dh[j], v) + e[v] + (last ? dhT.get(p, bits, j, c, v) : 0.0f), gs = g * si;
                 e[v] = a * g;
                 const float q = log2a[v] * sr * fmaf(e[v], w.u[j][v], -(a * ib) * (a * gs * x));
                 sum[v] += q;
@@ -584,6 +640,7 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
             rows.dh[j] = load_pack<T, V>(pd.at, off + pd.row_or_last(j));
         }
     }
+    const Ahead<V> h0(p, bits, bits.first, p.h0, c), dhT(p, bits, bits.last, p.dhT, c);
     float decay[V], A[V], S[V], D[V], h[V], e[V], sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -600,8 +657,8 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
             rows.a[j][v] = g.a; rows.sr[j][v] = g.sr; rows.si[j][v] = g.si; rows.b[j][v] = g.b;
             rows.u[j][v] = g.b * g.si * get<T, V>(rows.x[j], v);
         }
-    if (bits.plain) bwd_maps<T, V, TW, true>(p, bits, c, rows, A, S, D);
-    else bwd_maps<T, V, TW, false>(p, bits, c, rows, A, S, D);
+    if (bits.plain) bwd_maps<T, V, TW, true>(p, bits, c, rows, A, S, D, h0, dhT);
+    else bwd_maps<T, V, TW, false>(p, bits, c, rows, A, S, D, h0, dhT);
 #pragma unroll
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; mapD[wave][lane * V + v] = D[v]; }
     __syncthreads();
@@ -625,8 +682,8 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
     for (int w = 0; w < wave; ++w)
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(mapA[w][lane * V + v], h[v], mapS[w][lane * V + v]);
-    if (bits.plain) bwd_rows<T, V, TW, true>(p, bits, t0, c, off, decay, rows, h, e, sum);
-    else bwd_rows<T, V, TW, false>(p, bits, t0, c, off, decay, rows, h, e, sum);
+    if (bits.plain) bwd_rows<T, V, TW, true>(p, bits, t0, c, off, decay, rows, h, e, sum, h0, dhT);
+    else bwd_rows<T, V, TW, false>(p, bits, t0, c, off, decay, rows, h, e, sum, h0, dhT);
     if (p.dh0) pass_empty<V>(p, p.dhT, p.dh0, c, (long long)k * NW + wave, (long long)chunks * NW);
     __syncthreads();                                        // the maps have been read
 #pragma unroll
@@ -742,9 +799,10 @@ RecurPlan plan_of(const scan2d_recur_desc* d, int pass) {
     q.cols = (d->C + 64 * q.V - 1) / (64 * q.V);
     q.waves = pass == SCAN2D_PASS_BWD ? kBwdWaves : kFwdWaves;
     const auto chunks = [&](int rows) { return (d->T + rows * q.waves - 1) / (rows * q.waves); };
-    // forward, bf16: 16 rows of a wavefront (9001 x 1024 30 us, with 8 rows 37), but 8 where that leaves compute units without a
-    // workgroup (1000 x 512 10.1 us, with 16 rows 12.0; 37 x 256 5.8 and 8.9)
-    q.rows = pass == SCAN2D_PASS_BWD ? kBwdRows : d->dtype == SCAN2D_BF16 && chunks(16) * q.cols >= 256 ? 16 : 8;
+    // forward, bf16 or one channel a lane: 16 rows of a wavefront (9001 x 1024 30 us, with 8 rows 37), but 8 where that leaves compute units
+    // without a workgroup (1000 x 512 10.1 us, with 16 rows 12.0; 37 x 256 5.8 and 8.9), or with registers for too few (fp32)
+    const bool deep = d->dtype == SCAN2D_BF16 || q.V == 1;
+    q.rows = pass == SCAN2D_PASS_BWD ? kBwdRows : deep && chunks(16) * q.cols >= 256 ? 16 : 8;
     q.chunks = (int)chunks(q.rows);
     return q;
 }
@@ -785,7 +843,7 @@ int recur_fwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
     }
     using Kernel = void (*)(const RecurArgs, int, int);
     Kernel k;
-    if (d->dtype != SCAN2D_BF16) k = q.V == 1 ? recur_fwd_kernel<float, 1, 8, kFwdWaves> : recur_fwd_kernel<float, 2, 8, kFwdWaves>;
+    if (d->dtype != SCAN2D_BF16) k = q.V == 2 ? recur_fwd_kernel<float, 2, 8, kFwdWaves> : q.rows == 8 ? recur_fwd_kernel<float, 1, 8, kFwdWaves> : recur_fwd_kernel<float, 1, 16, kFwdWaves>;
     else if (q.rows == 8) k = q.V == 1 ? recur_fwd_kernel<bf16_t, 1, 8, kFwdWaves> : recur_fwd_kernel<bf16_t, 2, 8, kFwdWaves>;
     else k = q.V == 1 ? recur_fwd_kernel<bf16_t, 1, 16, kFwdWaves> : recur_fwd_kernel<bf16_t, 2, 16, kFwdWaves>;
     hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * q.waves), 0, stream, a, q.chunks, q.cols);
