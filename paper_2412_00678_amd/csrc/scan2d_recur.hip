@@ -7,18 +7,19 @@
 // A sequence of maps h -> A h + S composes to one of the same form: (A1, S1) then (A2, S2) is (A1 A2, A2 S1 + S2).  A
 // workgroup takes a chunk of TW x NW consecutive rows (of whatever sequences) x 64 V channels: a wavefront has TW
 // rows, a lane V neighbouring channels of them, all in registers.  Each lane forms the map of its rows, the wavefronts' maps
-// meet in LDS, and the chunk's map (A, S) goes to the workspace, where the chunks behind it pick it up.  The state in front
-// of a chunk is the one behind the last full group of kGroup chunks, which the group's last chunk has written, carried
-// through the maps of the chunks in between, always in this order: the same bits every time.  With the state in hand the lane runs its
-// rows once more from registers and writes them.  The first row of a sequence enters as A = -0, S = a h0 + u, rows of
+// meet in LDS, and the chunk's map (A, S) goes to the workspace, where the chunks behind it pick it up; the last chunk of a
+// team of kTeam writes the team's map instead, and the last of a group of kTeams teams the state behind the group.  The state in front
+// of a chunk is the one behind the group before, carried through the maps of the teams and chunks in between, always in this order: the
+// same bits every time.  With the state in hand the lane runs its rows once more from registers and writes them.  The first row of a sequence enters as A = -0, S = a h0 + u, rows of
 // no sequence as A = -0, S = 0, so sequences of any lengths share chunks; the sign marks a map that does not look at
-// what comes before it (0 times a NaN would), where a product of decays that underflows is +0.  The backward pass is the same scan from the last row to the first
-// for e_t = a_t (dh_t + e_{t+1}); it rebuilds the states from the ones in front of each chunk, which the forward saved.
+// what comes before it (0 times a NaN would), where a product of decays that underflows is +0.
+// The backward pass is the same scan from the last row to the first for e_t = a_t (dh_t + e_{t+1}); it rebuilds the states from the ones in front of each chunk, which the forward saved.
 //
-// No wait without an end: a workgroup draws its chunk from its columns' counter, so every chunk it waits for belongs to
-// a workgroup that is already running; a chunk's map is written before its workgroup waits for anything, and the state behind
-// a group needs only chunks with smaller numbers.  A word in the workspace holds value and flag together (one 64-bit
-// store), set to "not written" by a kernel in front of the pass.
+// No wait without an end: a workgroup draws its chunk from its column's counter, so every chunk with a smaller number belongs to
+// a workgroup that is already running; a chunk's map is written before its workgroup waits for anything, the map of a team and the state
+// behind a group wait for chunks with smaller numbers only.  A word in the workspace holds value and flag together (one 64-bit
+// store), set to "not written" by a kernel in front of the pass.  A workspace that two calls share at the same time breaks
+// all that; for them a wait ends after kSpins looks all the same, with NaN for what did not come, and chunks past the last are none.
 #include "scan2d_seq.hpp"
 
 #include "scan2d_block.hpp"
@@ -236,7 +237,8 @@ __device__ __forceinline__ void pass_empty(const RecurArgs& p, const float* from
 // ---- the chain of chunks
 // Workspace: a counter per column of workgroups (64 bytes each), then per chunk the maps (A, S) of its channels (behind the last chunk
 // of a team: of the whole team), then per group the states behind it.  All bits set: not written.
-constexpr uint32_t kUnset = 0xffffffffu;
+constexpr uint32_t kUnset = 0xffffffffu;                    // a NaN
+constexpr int kSpins = 1 << 20;          // looks at a word before it is given up: a second or two
 __host__ __device__ inline size_t chain_counters(int cols) { return (size_t)cols * 8; }               // in 64-bit words
 __host__ __device__ inline size_t chain_words(int chunks, int cols, int width) {
     return chain_counters(cols) + ((size_t)chunks + (size_t)(chunks + kGroup - 1) / kGroup) * cols * width;
@@ -275,14 +277,14 @@ __device__ __forceinline__ int chain_start(const RecurArgs& p, uint64_t* ws, int
 // Waits for the words of one chunk or group, V per lane.
 template <int V>
 __device__ __forceinline__ void chain_wait(const uint64_t* w, uint64_t* v) {
-    for (;;) {
+    for (int spin = 0;; ++spin) {
         bool all = true;
 #pragma unroll
         for (int q = 0; q < V; ++q) {
             v[q] = chain_get(w + q * 64);
             all = all && is_set(v[q]);
         }
-        if (__all(all)) return;
+        if (__all(all) || spin == kSpins) return;
         __builtin_amdgcn_s_sleep(4);
     }
 }
@@ -308,8 +310,8 @@ __device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int co
     // the first wavefront: the maps of the team in front of this chunk, to LDS
     const auto near = [&] {
         uint64_t w[kTeam - 1][V];
-        for (bool all = false; !all;) {
-            all = true;
+        for (int spin = 0;; ++spin) {
+            bool all = true;
 #pragma unroll
             for (int m = 0; m < kTeam - 1; ++m)
 #pragma unroll
@@ -320,8 +322,8 @@ __device__ __forceinline__ void chain(uint64_t* ws, int chunks, int cols, int co
                         all = all && is_set(w[m][v]);
                     }
                 }
-            all = __all(all);
-            if (!all) __builtin_amdgcn_s_sleep(4);
+            if (__all(all) || spin == kSpins) break;
+            __builtin_amdgcn_s_sleep(4);
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -479,6 +481,7 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
     uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
     const SeqSearch search(p);
     const int k = chain_start<V, NW>(p, ws, chunks, cols, col, lds);
+    if ((unsigned)k >= (unsigned)chunks) return;
     const int c = min(col * WIDTH + lane * V, p.C - V);     // the lanes past the last channels do those again
     const uint32_t off = (uint32_t)c * EB;
     const int t0 = (k * NW + wave) * TW;
@@ -621,6 +624,7 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
     uint64_t* const ws = static_cast<uint64_t*>(p.workspace);
     const SeqSearch search(p);
     const int n = chain_start<V, NW>(p, ws, chunks, cols, col, lds), k = chunks - 1 - n;   // the chain runs from the last chunk
+    if ((unsigned)n >= (unsigned)chunks) return;
     const int c = min(col * WIDTH + lane * V, p.C - V);
     const uint32_t off = (uint32_t)c * EB;
     const int t0 = (k * NW + wave) * TW;

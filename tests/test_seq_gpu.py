@@ -134,6 +134,14 @@ RECUR_CASES = [
     ("equal", [100] * 3, 100, 70, "bf16", {}),
     ("equal", [1] * 5, 1, 256, "fp32", {}),
     ("equal", [1000] * 2, 1000, 96, "fp32", {"gate": 8.0}),
+    # several groups of chunks, 16 rows of a wavefront, one and two channels of a lane
+    ("packed", [4150, 60], 0, 1030, "bf16", {}),
+    ("packed", [9000], 0, 70, "bf16", {"states": False}),
+    ("packed", [20011, 13000], 0, 40, "fp32", {}),
+    # more sequences than a wavefront has lanes, some of them long, and empty ones in a row
+    ("packed", [7, 0, 30, 1, 0, 0, 95, 2] * 25, 0, 90, "bf16", {"behind": 11}),
+    ("packed", [0] * 150 + [40] + [0] * 90 + [3], 0, 20, "fp32", {}),
+    ("padded", [0, 12, 3, 12, 7] * 30, 12, 68, "fp32", {}),
 ]
 
 
@@ -328,6 +336,25 @@ NORM_CASES = [
     (70, 20, 48, 6, "fp32", "gelu", True, True, {}),
     (1, 9000, 7, 7, "fp32", "silu", True, True, {}),
     (1, 20000, 64, 32, "fp32", "silu", True, True, {}),
+    # single rows: groups of many channels, odd ones, more rows than there are teams, channels below a load's width
+    (9, 1, 1306, 2, "bf16", "gelu", False, True, {}),
+    (33, 1, 1330, 1, "fp32", "silu", True, True, {"pad": (1, 0)}),
+    (40, 1, 2048, 1, "bf16", "silu", True, True, {}),
+    (21, 1, 2048, 1, "fp32", "none", False, True, {}),
+    (12, 1, 1536, 3, "fp32", "gelu", False, False, {}),
+    (5, 1, 2050, 1, "fp32", "silu", False, True, {}),
+    (3, 1, 4200, 2, "bf16", "silu", True, True, {}),
+    (5000, 1, 512, 8, "bf16", "silu", True, True, {}),
+    (9001, 1, 33, 3, "fp32", "none", False, True, {}),
+    (6, 1, 3, 1, "fp32", "silu", False, True, {}),
+    (6, 1, 5, 1, "bf16", "none", False, True, {}),
+    # a few positions, narrow and wide groups, slabs of a part of the row and of a part of a group
+    (2, 9, 2, 1, "bf16", "silu", True, True, {}),
+    (130, 2, 40, 4, "fp32", "silu", False, True, {}),
+    (2, 700, 1602, 2, "bf16", "silu", True, True, {}),
+    (1, 3000, 596, 1, "fp32", "gelu", True, True, {}),
+    (3, 3, 4200, 2, "fp32", "none", False, True, {}),
+    (1, 1500, 2600, 1, "bf16", "silu", True, True, {}),
 ]
 
 
@@ -410,7 +437,7 @@ def test_group_norm_of_a_large_mean_keeps_its_variance(torch, s2d, P):
 
 def test_group_norm_in_place(torch, s2d):
     rng = np.random.default_rng(17)
-    for shape in ((3, 50, 40), (1, 9000, 40), (50, 1, 320)):
+    for shape in ((3, 50, 40), (1, 9000, 40), (50, 1, 320), (5000, 1, 36), (7, 1, 1100), (3, 5, 4100)):
         x, dy = rows(torch, rng, shape, "bf16"), rows(torch, rng, shape, "bf16")
         y, stats = s2d.group_norm_fwd(x, None, None, 4, act=s2d.ACT_SILU)
         dx, _, _ = s2d.group_norm_bwd(x, None, None, 4, stats, dy, act=s2d.ACT_SILU)
