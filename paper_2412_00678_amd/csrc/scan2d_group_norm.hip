@@ -640,7 +640,10 @@ __global__ __launch_bounds__(kTokenThreads) void group_norm_tokens_bwd_kernel(co
     for (int j = 0; j < J; ++j) {
         load_params<V>(p, l.c[j], gamma[j], beta[j]);
 #pragma unroll
-        for (int v = 0; v < V; ++v) accb[j][v] = accg[j][v] = 0.0f;
+        for (int v = 0; v < V; ++v) {
+            gamma[j][v] = l.own(j, v) ? gamma[j][v] : 0.0f; // 0 times another group's infinity would count below
+            accb[j][v] = accg[j][v] = 0.0f;
+        }
     }
     const float inv = 1.0f / (float)q.D;
     for (long long it = 0; it * R * step < p.N; ++it, n0 += R * step) {

@@ -630,3 +630,26 @@ def test_binding_refusals(torch, s2d):
         with pytest.raises(s2d.Scan2dError) as e:
             s2d.group_norm_fwd(**{**dict(x=m, gamma=None, beta=None, groups=2), **bad})
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("P", [1, 9, 4000])
+@pytest.mark.parametrize("C,G,dtype", [(18, 3, "fp32"), (36, 3, "fp32"), (72, 3, "bf16"), (1194, 2, "bf16")])
+def test_group_norm_infinite_gamma_stays_in_its_group(torch, s2d, P, C, G, dtype):
+    """A weight that is infinite or NaN spoils its own group only: the others keep their bits."""
+    rng = np.random.default_rng(P + C)
+    N, D = (3, C // G)
+    x, dy = (rows(torch, rng, (N, P, C), dtype) for _ in range(2))
+    beta = torch.zeros(C, device="cuda")
+    results = []
+    for bad in (1.0, float("inf"), float("nan")):
+        gamma = torch.ones(C, device="cuda")
+        gamma[0] = gamma[D - 1] = gamma[C - D] = bad             # of the first and the last group
+        if G == 2:
+            gamma[C - D:] = 1.0                                  # two groups: the first only
+        y, stats = s2d.group_norm_fwd(x, gamma, beta, G, act=s2d.ACT_SILU)
+        results.append((y, stats, *s2d.group_norm_bwd(x, gamma, beta, G, stats, dy, act=s2d.ACT_SILU)))
+    well = slice(D, 2 * D)
+    for got in results[1:]:
+        for a, b in zip(results[0], got):
+            keep = (..., slice(1, 2), slice(None)) if a is results[0][1] else (..., well)
+            assert torch.equal(a[keep], b[keep])
