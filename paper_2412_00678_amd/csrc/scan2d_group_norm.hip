@@ -260,7 +260,7 @@ __global__ __launch_bounds__(TH) void group_norm_fwd_kernel(const GroupNormArgs 
     float* const myred = red + R * base * PER;
     float gamma[V], beta[V];
     load_params<V>(p, l.c, gamma, beta);
-    const int step = teams / q.slabs, rounds = (p.N + step * R - 1) / (step * R);
+    const int step = teams / q.slabs, rounds = (p.N - 1) / (step * R) + 1;
     for (int it = 0; it < rounds; ++it) {
         Pack<T, V> x[R][K];
         bool live[R][K];
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
     load_params<V>(p, l.c, gamma, beta);
 #pragma unroll
     for (int v = 0; v < V; ++v) accb[v] = accg[v] = 0.0f;
-    const int step = teams / q.slabs, rounds = (p.N + step * R - 1) / (step * R);
+    const int step = teams / q.slabs, rounds = (p.N - 1) / (step * R) + 1;
     for (int it = 0; it < rounds; ++it) {
         Pack<T, V> x[R][K], dy[R][K];
         bool live[R][K], real[R];
@@ -753,7 +753,7 @@ struct Tile {
         chunk = r % chunks;
         n = r / chunks;
         r0 = chunk * per;
-        r1 = min(r0 + per, P);
+        r1 = P - r0 < per ? P : r0 + per;                   // r0 + per may pass 2^31
     }
 };
 // kRows rows of a lane from r on: what they hold, and which of them count

@@ -653,3 +653,32 @@ def test_group_norm_infinite_gamma_stays_in_its_group(torch, s2d, P, C, G, dtype
         for a, b in zip(results[0], got):
             keep = (..., slice(1, 2), slice(None)) if a is results[0][1] else (..., well)
             assert torch.equal(a[keep], b[keep])
+
+
+def test_group_norm_of_as_many_rows_as_there_may_be(torch, s2d):
+    """2^31 - 4100 rows, as one item's positions and as items of one: the last rows are done too."""
+    rows_, last = 2 ** 31 - 4100, 2 ** 23
+    pattern = torch.tensor([1.0, 3.0, -2.0, 0.5, -0.5, 4.0], dtype=torch.bfloat16, device="cuda")      # whole patterns: the rows are a multiple of 6
+    x = pattern.repeat(rows_ // 6 + 1)[:rows_].reshape(1, rows_, 1)
+    y, stats = s2d.group_norm_fwd(x, None, None, 1)
+    torch.cuda.synchronize()
+    mean, var = 1.0, float(pattern.double().var(unbiased=False))
+    # a lane joins its 2^13 rows four at a time, 2^11 roundings of 2^-24 of a mean (1) and of a sum of squares
+    assert abs(float(stats[0, 0, 0]) - mean) < 2.0 ** -12 and abs(float(stats[0, 0, 1]) * var ** 0.5 - 1.0) < 2.0 ** -12
+    tail = (x[0, -last:, 0].float() - stats[0, 0, 0]) * stats[0, 0, 1]
+    assert float((y[0, -last:, 0].float() - tail).abs().max()) <= 2.0 ** -8 * 2.0
+    dx, dgamma, _ = s2d.group_norm_bwd(x, torch.ones(1, device="cuda"), None, 1, stats, y)
+    torch.cuda.synchronize()
+    # dy = y: sum dv = 0, sum dv xh = the rows, so dx = 0 up to the rounding of y to bf16
+    assert float(dx[0, -last:].float().abs().max()) <= 2.0 ** -7 * 2.0
+    assert abs(float(dgamma[0]) / rows_ - 1.0) < 2.0 ** -7
+    del y, dx
+    x = x.reshape(rows_, 1, 1)
+    gamma, beta = torch.ones(1, device="cuda"), torch.tensor([0.75], device="cuda")
+    y, stats = s2d.group_norm_fwd(x, gamma, beta, 1, eps=1.0)
+    torch.cuda.synchronize()
+    assert torch.equal(stats[-last:, 0, 0], x[-last:, 0, 0].float()) and bool((stats[-last:, 0, 1] == 1.0).all())
+    assert bool((y[-last:] == 0.75).all())
+    dx, dgamma, dbeta = s2d.group_norm_bwd(x, gamma, beta, 1, stats, y, dx=y)
+    torch.cuda.synchronize()
+    assert bool((dx[-last:] == 0).all()) and abs(float(dbeta[0]) / rows_ - 0.75) < 1e-5 and float(dgamma[0]) == 0.0
