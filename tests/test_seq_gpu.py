@@ -682,3 +682,28 @@ def test_group_norm_of_as_many_rows_as_there_may_be(torch, s2d):
     dx, dgamma, dbeta = s2d.group_norm_bwd(x, gamma, beta, 1, stats, y, dx=y)
     torch.cuda.synchronize()
     assert bool((dx[-last:] == 0).all()) and abs(float(dbeta[0]) / rows_ - 0.75) < 1e-5 and float(dgamma[0]) == 0.0
+
+
+@pytest.mark.parametrize("T", [256, 257, 1027, 5002])
+def test_step_finds_a_slot_again_wherever_it_stands(torch, s2d, T):
+    """Two rows of one slot at any distance, the table at any 4-byte address: as one call after the other."""
+    rng = np.random.default_rng(T)
+    C = 3
+    x, r, i = (rows(torch, rng, (T, C), "fp32") for _ in range(3))
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    table = rng.permutation(T + 40).astype(np.int32)[:T]
+    pairs = [(0, T - 1), (1, T // 2), (T // 3, T - 2), (T - 4, T - 3)]
+    for a, b in pairs:
+        table[b] = table[a]
+    slots = torch.from_numpy(np.concatenate([[0], table]).astype(np.int32)).cuda()[1:]
+    pool = torch.from_numpy(rng.normal(size=(T + 40, C)).astype(np.float32)).cuda()
+    state, one = pool.clone(), pool.clone()
+    h = s2d.seq_recur_step(x, r, i, lam, state, slots=slots)
+    later = [b for _, b in pairs]
+    early = [t for t in range(T) if t not in later]
+    each = torch.empty_like(h)
+    for part in (early, later):                              # no slot twice in either
+        part = torch.tensor(part, device="cuda")
+        each[part] = s2d.seq_recur_step(x[part], r[part], i[part], lam, one, slots=slots[part])
+    torch.cuda.synchronize()
+    assert torch.equal(state, one) and torch.equal(h, each)
