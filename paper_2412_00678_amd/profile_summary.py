@@ -2,7 +2,7 @@
 
     python -m paper_2412_00678_amd.profile_summary commands RUNS   # prints the rocprofv3 command lines, one per run
     python -m paper_2412_00678_amd.profile_summary write RUNS      # reads RUNS/*, writes profiles/*.md and profiles/traffic.json
-    python -m paper_2412_00678_amd.profile_summary case NAME N     # runs a listed case of perf/cases.py N times (traced by `commands`)
+    python -m paper_2412_00678_amd.profile_summary case NAME N     # runs a listed case of perf/cases.py or perf/operators.py N times
 
 `commands` prints one shell line per run (kernel trace, FETCH_SIZE, WRITE_SIZE and issue counters, each a run
 of its own, plus the copy-kernel runs that calibrate the two size counters); run them on the GPU from /tmp with
@@ -34,6 +34,12 @@ PMC_STEPS = {1: "--steps 20 --warmup 4", 2: "--steps 20 --warmup 4", 3: "--steps
 CASES = (("train_14x14_fp32_b8", 300), ("train_gated_56x56_bf16_b32", 60), ("train_gated_211x397_bf16_mask", 30), ("block_14x14_bf16_b8", 200),
          ("slide_57x83_bf16_mask", 200), ("slide_127x201_fp32_mask", 100))
 
+# cases of perf/operators.py (the sequence layers), and those whose bytes are counted too
+SEQ_CASES = (("recur_fwd_37x256_bf16", 100), ("recur_fwd_packed_9001x1024_bf16", 100), ("recur_fwd_65536x2048_bf16", 20), ("recur_train_16384x2048_bf16", 20),
+             ("recur_train_5003x771_fp32", 60), ("recur_step_384x2048_bf16", 100), ("norm_fwd_8x14x14x256_bf16", 100), ("norm_fwd_32x56x56x192_bf16", 60),
+             ("norm_train_1x256x256x256_bf16_mask", 60), ("norm_train_3x57x83x384_fp32", 60), ("norm_train_16384x1x2048_bf16", 40))
+SEQ_BYTES = ("recur_fwd_65536x2048_bf16", "recur_train_16384x2048_bf16", "norm_train_1x256x256x256_bf16_mask", "norm_train_16384x1x2048_bf16")
+
 
 def runs():
     out = []
@@ -57,6 +63,11 @@ def runs():
         out.append((f"plain_producers_{w}", None, b, f"plain_producers_{w}.json"))
     for name, passes in CASES:
         out.append((f"trace_case_{name}", "--kernel-trace --stats", f"python3 ./paper_2412_00678_amd/profile_summary.py case {name} {passes}", None))
+    for name, passes in SEQ_CASES:
+        prog = "python3 ./paper_2412_00678_amd/profile_summary.py case"
+        out.append((f"trace_case_{name}", "--kernel-trace --stats", f"{prog} {name} {passes}", None))
+        if name in SEQ_BYTES:
+            out += [(f"{c.lower()}_case_{name}", f"--pmc {c}_SIZE", f"{prog} {name} 6", None) for c in ("FETCH", "WRITE")]
     out.append(("fetch_copy", "--pmc FETCH_SIZE", "./paper_2412_00678_amd/roofprobe --copy 5", None))
     out.append(("write_copy", "--pmc WRITE_SIZE", "./paper_2412_00678_amd/roofprobe --copy 5", None))
     return out
@@ -212,7 +223,8 @@ def raw_counter_table(runs_dir, name):
 
 # sources that the recorded workloads (scan2d_fwd / scan2d_bwd on the benchmark configurations) do not run: the probe
 # and the layers around the scan
-NOT_IN_DIGEST = ("roofprobe", "scan2d_block", "scan2d_contract", "scan2d_xproj", "scan2d_pool", "scan2d_linear", "scan2d_norm")
+NOT_IN_DIGEST = ("roofprobe", "scan2d_block", "scan2d_contract", "scan2d_xproj", "scan2d_pool", "scan2d_linear", "scan2d_norm",
+                 "scan2d_seq", "scan2d_recur", "scan2d_group_norm")
 
 
 def kernel_source_digest() -> str:
@@ -414,7 +426,11 @@ def run_case(name, passes):
     """`passes` passes of a listed case over two states in turn, as a program's loop over its data would run them."""
     sys.path.insert(0, ROOT)
     import torch
-    from perf import cases
+    if any(name == n for n, _ in SEQ_CASES):
+        from perf import operators as cases
+        cases.own = True
+    else:
+        from perf import cases
     case = next(c for c in cases.listed() if c["name"] == name)
     states = [cases.prepare(case, seed) for seed in (1, 2)]
     torch.cuda.synchronize()
@@ -430,6 +446,26 @@ def write_cases(runs_dir, by_name):
         for name, passes in CASES:
             run = f"trace_case_{name}"
             f.write(f"\n## {name}, {passes} passes\n\n`{shown(by_name[run])}`\n\n{kernel_table(runs_dir, run, '%scan2d%')}\n")
+
+
+def write_sequence(runs_dir, by_name):
+    from perf import operators
+    with open(os.path.join(PROFILES, "sequence_layers.md"), "w") as f:
+        f.write("# Kernels of the sequence layers (gated linear recurrence, group norm) in the cases of `perf/operators.py`\n\n"
+                "Each run makes two states and passes over them in turn.  Averages are under the tracer, which lengthens short kernels.  Bytes: all\n"
+                "kernels of a pass together, read from and written to HBM (FETCH_SIZE, WRITE_SIZE, scaled by the copy whose bytes are known), beside the\n"
+                "least that the operator has to move.\n")
+        fs, ws, _, _ = copy_scales(runs_dir)
+        for name, passes in SEQ_CASES:
+            run = f"trace_case_{name}"
+            f.write(f"\n## {name}, {passes} passes\n\n`{shown(by_name[run])}`\n\n{kernel_table(runs_dir, run, '%scan2d%')}\n")
+            if name in SEQ_BYTES:
+                least = operators.work(next(c for c in operators.listed() if c["name"] == name))["bytes"]
+                mb = []
+                for c, scale in (("FETCH", fs), ("WRITE", ws)):
+                    per = counters(runs_dir, f"{c.lower()}_case_{name}")
+                    mb.append(sum(v[f"{c}_SIZE"][0] * v[f"{c}_SIZE"][1] for v in per.values()) / 6 * scale * 1024 / 1e6)
+                f.write(f"\nHBM per pass: {mb[0]:.1f} MB read, {mb[1]:.1f} MB written; least: {least / 1e6:.1f} MB in all\n")
 
 
 def main(argv):
@@ -448,6 +484,7 @@ def main(argv):
     write(runs_dir)
     write_producers(runs_dir, {r[0]: r for r in runs()})
     write_cases(runs_dir, {r[0]: r for r in runs()})
+    write_sequence(runs_dir, {r[0]: r for r in runs()})
     return 0
 
 
