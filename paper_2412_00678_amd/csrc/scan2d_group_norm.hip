@@ -16,6 +16,10 @@
 // Backward: the channels' sums of dv and dv xh of a tile, joined to those of the item and with gamma to the groups', then dx from a second read.
 // The variance is always taken from deviations, never from the difference of two large sums.
 // All sums run in a fixed order.
+//
+// Measured (forward, backward; a copy reaches 5.2 TB/s, 8.6 where it stays in the Infinity Cache): 16384 tokens x 2048 bf16 31 and 52 us (4.3 and 3.9 TB/s of their
+// bytes), held 8 x 196 x 256 bf16 7.4 and 10.7 us, split 65536 x 256 bf16 masked 30 and 44 us, 32 x 3136 x 192 bf16 31 and 46 us, 3 x 4731 x 384 fp32
+// 20 and 30 us.  What the split form adds to the bytes' time: the second read, out of the Infinity Cache, and 3 to 5 us per launch.
 #include "scan2d_seq.hpp"
 
 #include "scan2d_block.hpp"

@@ -1,4 +1,5 @@
-"""Thin binding of the C-ABI library `libscan2d.so` (see include/scan2d.h).
+"""Thin binding of the C-ABI library `libscan2d.so` (see include/scan2d.h, and include/scan2d_seq.h for the sequence
+layers: `seq_recur_*`, `group_norm_*`).
 
 Argument marshalling only: every step of the scan runs in the HIP kernels.  PyTorch is used
 for device memory and the current stream, nothing else.  The calls of a program's inner loop
