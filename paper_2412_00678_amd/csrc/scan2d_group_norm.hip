@@ -18,7 +18,7 @@
 // All sums run in a fixed order.
 //
 // Measured (forward, backward; a copy reaches 5.2 TB/s, 8.6 where it stays in the Infinity Cache): 16384 tokens x 2048 bf16 31 and 52 us (4.3 and 3.9 TB/s of their
-// bytes), held 8 x 196 x 256 bf16 7.4 and 10.7 us, split 65536 x 256 bf16 masked 30 and 44 us, 32 x 3136 x 192 bf16 31 and 46 us, 3 x 4731 x 384 fp32
+// bytes), held 8 x 196 x 256 bf16 7.4 and 10.7 us, split 65536 x 256 bf16 masked 25 and 40 us, 32 x 3136 x 192 bf16 28 and 45 us, 3 x 4731 x 384 fp32
 // 20 and 30 us.  What the split form adds to the bytes' time: the second read, out of the Infinity Cache, and 3 to 5 us per launch.
 #include "scan2d_seq.hpp"
 
@@ -760,21 +760,42 @@ struct Tile {
         r1 = P - r0 < per ? P : r0 + per;                   // r0 + per may pass 2^31
     }
 };
-// kRows rows of a lane from r on: what they hold, and which of them count
-template <typename T, int V, bool ONE>
-__device__ __forceinline__ void load_rows(const void* x, long long sx, const uint8_t* mask, const Geo& q, const Lane<V, ONE>& l, const Tile& t, long long row0, int r,
-                                          Pack<T, V>* to, bool* live) {
+// kRows rows of a lane from r on: their masks, and what the ones that count hold (the others are not read: 65536 x 256 bf16 with half of
+// the positions masked, forward and backward 74 us where all are read, 66 so).  A batch's masks are asked for a batch ahead.
+template <bool MASK>
+struct Rows {
+    uint8_t mask[kRows];
+    bool live[kRows];
+    template <typename L>
+    __device__ __forceinline__ void ask(const uint8_t* masks, const Geo& q, const L& l, const Tile& t, long long row0, int r) {
+        if constexpr (MASK) {
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-        const int at = r + l.slot + k * q.slots;
-        const long long row = row0 + min(at, t.r1 - 1);
-        to[k] = load_pack<T, V>(static_cast<const T*>(x) + row * sx + l.c);
-        if (live) live[k] = l.on && at < t.r1 && (mask == nullptr || mask[row] == 0);
+            for (int k = 0; k < kRows; ++k) mask[k] = masks[row0 + min(r + l.slot + k * q.slots, t.r1 - 1)];
+        }
     }
-}
+    template <typename L>
+    __device__ __forceinline__ void take(const Geo& q, const L& l, const Tile& t, int r) {
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) live[k] = l.on && r + l.slot + k * q.slots < t.r1 && (!MASK || mask[k] == 0);
+    }
+    template <typename T, int V, typename L>
+    __device__ __forceinline__ void load(const void* x, long long sx, const Geo& q, const L& l, const Tile& t, long long row0, int r, Pack<T, V>* to) const {
+        const T* const at = static_cast<const T*>(x) + l.c;
+        if constexpr (MASK) {
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) {
+                to[k] = Pack<T, V>();
+                if (live[k]) to[k] = load_pack<T, V>(at + (row0 + r + l.slot + k * q.slots) * sx);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) to[k] = load_pack<T, V>(at + (row0 + min(r + l.slot + k * q.slots, t.r1 - 1)) * sx);
+        }
+    }
+};
 
 // part[(n G + g) E + e] = (values, mean, squared deviations), E = chunks x spg tiles of a group
-template <typename T, int V, bool ONE>
+template <typename T, int V, bool ONE, bool MASK>
 __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float4* part) {
     constexpr int PER = ONE ? 1 : V;
     __shared__ float red[kTileThreads * PER], mean_of[kTileThreads * Lane<V, ONE>::GV];
@@ -787,10 +808,14 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const Gr
     for (int v = 0; v < V; ++v) mean[v] = m2[v] = 0.0f;
     int mine = 0;
     const int batch = q.slots * kRows;
+    Rows<MASK> rows_at;
+    const bool (&live)[kRows] = rows_at.live;
+    rows_at.ask(p.mask, q, l, t, row0, t.r0);
     for (int r = t.r0; r < t.r1; r += batch) {
         Pack<T, V> x[kRows];
-        bool live[kRows];
-        load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+        rows_at.take(q, l, t, r);
+        rows_at.template load<T, V>(p.x, p.sx, q, l, t, row0, r, x);
+        if (r + batch < t.r1) rows_at.ask(p.mask, q, l, t, row0, r + batch);
         int here = 0;
 #pragma unroll
         for (int k = 0; k < kRows; ++k) here += live[k];
@@ -813,7 +838,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const Gr
         }
         n += m;
     }
-    const int rows = p.mask != nullptr ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
+    const int rows = MASK ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
     const float M = (float)rows * (float)l.D, inv = rows > 0 ? 1.0f / M : 0.0f;
     float s[1][V];
 #pragma unroll
@@ -853,7 +878,7 @@ __global__ __launch_bounds__(64) void group_norm_join_kernel(const float4* part,
 }
 
 // part: the tiles, to be joined here, or null: the statistics are there.
-template <typename T, int V, bool ONE, int ACT>
+template <typename T, int V, bool ONE, bool MASK, int ACT>
 __global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, const float4* part) {
     constexpr int GV = Lane<V, ONE>::GV;
     __shared__ float2 joined[kTileThreads * GV];
@@ -862,10 +887,14 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const Gr
     const long long row0 = t.n * p.P;
     const int batch = q.slots * kRows, last = t.r0 + (t.r1 - 1 - t.r0) / batch * batch;
     Pack<T, V> x[kRows];
-    bool live[kRows];
-    load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, last, x, live);
+    Rows<MASK> rows_at;
+    const bool (&live)[kRows] = rows_at.live;
+    rows_at.ask(p.mask, q, l, t, row0, last);
     float gamma[V], beta[V], mean[GV], rstd[GV];
     load_params<V>(p, l.c, gamma, beta);
+    rows_at.take(q, l, t, last);
+    rows_at.template load<T, V>(p.x, p.sx, q, l, t, row0, last, x);
+    if (last > t.r0) rows_at.ask(p.mask, q, l, t, row0, last - batch);
     if (part != nullptr) {
         const int E = chunks * q.spg;
         for (int g = l.lt / q.tpg; g < l.groups; g += kTileThreads / q.tpg) {
@@ -886,7 +915,11 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const Gr
     }
     if (!l.on) return;
     for (int r = last; r >= t.r0; r -= batch) {
-        if (r < last) load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
+        if (r < last) {
+            rows_at.take(q, l, t, r);
+            rows_at.template load<T, V>(p.x, p.sx, q, l, t, row0, r, x);
+            if (r > t.r0) rows_at.ask(p.mask, q, l, t, row0, r - batch);
+        }
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             const int at = r + l.slot + k * q.slots;
@@ -902,7 +935,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const Gr
 }
 
 // sums[n][chunk][C] = (sum dv, sum dv xh) of a tile; counts[n][chunk]: its rows that count
-template <typename T, int V, bool ONE, int ACT>
+template <typename T, int V, bool ONE, bool MASK, int ACT>
 __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float2* sums, float* counts) {
     constexpr int GV = Lane<V, ONE>::GV;
     __shared__ float red[2][kTileThreads * V];
@@ -912,11 +945,18 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
     const long long row0 = t.n * p.P;
     const int batch = q.slots * kRows;
     Pack<T, V> x[kRows], dy[kRows];
-    bool live[kRows];
-    load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, t.r0, x, live);
-    load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, t.r0, dy, nullptr);
+    Rows<MASK> rows_at;
+    const bool (&live)[kRows] = rows_at.live;
+    rows_at.ask(p.mask, q, l, t, row0, t.r0);
     float gamma[V], beta[V], mean[GV], rstd[GV], b[V], g[V];
     load_params<V>(p, l.c, gamma, beta);
+    const auto load = [&](int r) {
+        rows_at.take(q, l, t, r);
+        rows_at.template load<T, V>(p.x, p.sx, q, l, t, row0, r, x);
+        rows_at.template load<T, V>(p.dy, p.sdy, q, l, t, row0, r, dy);
+        if (r + batch < t.r1) rows_at.ask(p.mask, q, l, t, row0, r + batch);
+    };
+    load(t.r0);
 #pragma unroll
     for (int v = 0; v < GV; ++v) {
         const float* st = p.stats + ((size_t)t.n * p.G + l.g0 + l.gr[v]) * 2;
@@ -927,10 +967,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
     for (int v = 0; v < V; ++v) b[v] = g[v] = 0.0f;
     int mine = 0;
     for (int r = t.r0; r < t.r1; r += batch) {
-        if (r > t.r0) {
-            load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
-            load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
-        }
+        if (r > t.r0) load(r);
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             mine += live[k];
@@ -949,7 +986,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
             red[0][l.slot * l.width + l.c + v - l.lo] = b[v];
             red[1][l.slot * l.width + l.c + v - l.lo] = g[v];
         }
-    const int rows = p.mask != nullptr ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
+    const int rows = MASK ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
     __syncthreads();
     for (int c = l.lt; c < l.width; c += kTileThreads) {
         float sb = 0.0f, sg = 0.0f;
@@ -1053,7 +1090,7 @@ __global__ __launch_bounds__(kJoinThreads) void group_norm_wide_coef_kernel(cons
 }
 
 // The workgroups behind the tiles' join the items' sums to dbeta and dgamma.
-template <typename T, int V, bool ONE, int ACT>
+template <typename T, int V, bool ONE, bool MASK, int ACT>
 __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, const float2* coef, unsigned tiles,
                                                                        const float2* chan) {
     constexpr int GV = Lane<V, ONE>::GV;
@@ -1068,11 +1105,18 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const Gro
     const long long row0 = t.n * p.P;
     const int batch = q.slots * kRows, last = t.r0 + (t.r1 - 1 - t.r0) / batch * batch;
     Pack<T, V> x[kRows], dy[kRows];
-    bool live[kRows];
-    load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, last, x, live);
-    load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, last, dy, nullptr);
+    Rows<MASK> rows_at;
+    const bool (&live)[kRows] = rows_at.live;
+    rows_at.ask(p.mask, q, l, t, row0, last);
     float gamma[V], beta[V], mean[GV], rstd[GV], s1[GV], s2[GV];
     load_params<V>(p, l.c, gamma, beta);
+    const auto load = [&](int r) {
+        rows_at.take(q, l, t, r);
+        rows_at.template load<T, V>(p.x, p.sx, q, l, t, row0, r, x);
+        rows_at.template load<T, V>(p.dy, p.sdy, q, l, t, row0, r, dy);
+        if (r > t.r0) rows_at.ask(p.mask, q, l, t, row0, r - batch);
+    };
+    load(last);
 #pragma unroll
     for (int v = 0; v < GV; ++v) {
         const size_t at = (size_t)t.n * p.G + l.g0 + l.gr[v];
@@ -1082,10 +1126,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const Gro
         s2[v] = coef[at].y;
     }
     for (int r = last; r >= t.r0; r -= batch) {
-        if (r < last) {
-            load_rows<T, V>(p.x, p.sx, p.mask, q, l, t, row0, r, x, live);
-            load_rows<T, V>(p.dy, p.sdy, p.mask, q, l, t, row0, r, dy, nullptr);
-        }
+        if (r < last) load(r);
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             const int at = r + l.slot + k * q.slots;
@@ -1208,11 +1249,13 @@ NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
         if ((long long)n.q.slots * kHeldRows >= d->P) return held(FORM_GROUP, kMaxWgs);
     }
     n.form = FORM_SPLIT;
-    // whole rows, or narrower slabs where they keep more lanes busy (1192 channels in two groups: 298 of 512, 447 with a group a slab)
+    // whole rows, or narrower slabs where they keep more lanes busy: 1.2 times (9 x 3000 x 1280 in 32 groups, bf16: 320 of 512 lanes 54 and 103 us, 480 41 and
+    // 80), 1.5 times where that cuts a group, whose parts are joined and whose rows share cache lines with another workgroup's (3 x 17280 x 516 in two: 63 and
+    // 83 us cut, 41 and 59 whole)
     (void)fill_geo(d, n.V, kTileThreads, kTileThreads * n.V, false, &n.q);
     for (int most = kTileThreads * n.V / 2; most >= 128; most /= 2) {
         Geo q;
-        if (fill_geo(d, n.V, kTileThreads, most, false, &q) && q.slots * q.width * 10 > n.q.slots * n.q.width * 11) n.q = q;
+        if (fill_geo(d, n.V, kTileThreads, most, false, &q) && q.slots * q.width * 10 >= n.q.slots * n.q.width * (q.spg > n.q.spg ? 15 : 12)) n.q = q;
     }
     const long long batch = (long long)n.q.slots * kRows, batches = (d->P + batch - 1) / batch, each = (long long)d->N * n.q.slabs;
     long long chunks = (kTileWgs + each - 1) / each;
@@ -1243,16 +1286,16 @@ int fwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams);
     return launched();
 }
-template <typename T, int V, bool ONE, int ACT>
+template <typename T, int V, bool ONE, int ACT, bool MASK>
 int fwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const long long blocks = (long long)a.N * n.chunks * n.q.slabs, groups = (long long)a.N * a.G;
     if (!launch_fits(blocks, kTileThreads) || !launch_fits(groups, 64)) return SCAN2D_ERR_BAD_SHAPE;
     float4* part = static_cast<float4*>(a.workspace);
     const bool in_apply = join_in_apply(n);
-    hipLaunchKernelGGL((group_norm_tiles_kernel<T, V, ONE>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, part);
+    hipLaunchKernelGGL((group_norm_tiles_kernel<T, V, ONE, MASK>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, part);
     if (!in_apply)
         hipLaunchKernelGGL(group_norm_join_kernel, dim3((unsigned)groups), dim3(64), 0, stream, part, n.chunks * n.q.spg, a.eps, a.stats);
-    hipLaunchKernelGGL((group_norm_apply_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, in_apply ? part : nullptr);
+    hipLaunchKernelGGL((group_norm_apply_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, in_apply ? part : nullptr);
     return launched();
 }
 template <typename T, int V, bool ONE, int ACT>
@@ -1273,7 +1316,7 @@ int bwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     if (params) hipLaunchKernelGGL(group_norm_params_kernel, dim3(cols), dim3(1024), 0, stream, parts, (int)n.parts, a.C, a.dgamma, a.dbeta);
     return launched();
 }
-template <typename T, int V, bool ONE, int ACT>
+template <typename T, int V, bool ONE, int ACT, bool MASK>
 int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
     const unsigned cols = (a.C + 15) / 16;
@@ -1291,7 +1334,7 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     w += up((size_t)a.N * a.C * sizeof(float2));
     float2* coef = reinterpret_cast<float2*>(w);
     const bool several = params && a.N > 1;
-    hipLaunchKernelGGL((group_norm_sums_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, sums, counts);
+    hipLaunchKernelGGL((group_norm_sums_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, sums, counts);
     float *const dgamma = several ? nullptr : a.dgamma, *const dbeta = several ? nullptr : a.dbeta;
     if (narrow) {
         hipLaunchKernelGGL(group_norm_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, a.C, a.G, a.D, gw, a.gamma,
@@ -1300,7 +1343,7 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
         hipLaunchKernelGGL(group_norm_wide_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, n.chunks, a.C, chan, dgamma, dbeta);
         hipLaunchKernelGGL(group_norm_wide_coef_kernel, dim3((unsigned)groups), dim3(kJoinThreads), 0, stream, chan, counts, n.chunks, a.G, a.D, a.gamma, coef);
     }
-    hipLaunchKernelGGL((group_norm_grad_kernel<T, V, ONE, ACT>), dim3((unsigned)blocks + (several ? cols : 0)), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, coef,
+    hipLaunchKernelGGL((group_norm_grad_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks + (several ? cols : 0)), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, coef,
                        (unsigned)blocks, chan);
     return launched();
 }
@@ -1332,8 +1375,9 @@ int run(const GroupNormArgs& a, const NormPlan& n, bool backward, hipStream_t st
             }
         }
     } else if constexpr (V <= 4) {                          // eight channels of a lane: single rows only
-        if (backward) return n.form == FORM_SPLIT ? bwd_split<T, V, ONE, ACT>(a, n, stream) : bwd_held<T, V, ONE, ACT>(a, n, stream);
-        return n.form == FORM_SPLIT ? fwd_split<T, V, ONE, ACT>(a, n, stream) : fwd_held<T, V, ONE, ACT>(a, n, stream);
+        if (n.form != FORM_SPLIT) return backward ? bwd_held<T, V, ONE, ACT>(a, n, stream) : fwd_held<T, V, ONE, ACT>(a, n, stream);
+        if (a.mask != nullptr) return backward ? bwd_split<T, V, ONE, ACT, true>(a, n, stream) : fwd_split<T, V, ONE, ACT, true>(a, n, stream);
+        return backward ? bwd_split<T, V, ONE, ACT, false>(a, n, stream) : fwd_split<T, V, ONE, ACT, false>(a, n, stream);
     }
     return SCAN2D_ERR_BAD_SHAPE;
 }
