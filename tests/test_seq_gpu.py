@@ -707,3 +707,34 @@ def test_step_finds_a_slot_again_wherever_it_stands(torch, s2d, T):
         each[part] = s2d.seq_recur_step(x[part], r[part], i[part], lam, one, slots=slots[part])
     torch.cuda.synchronize()
     assert torch.equal(state, one) and torch.equal(h, each)
+
+
+@pytest.mark.parametrize("N,P,C,G,dtype,act,share,affine", [
+    (1, 2500, 130, 2, "bf16", "silu", 0.5, True), (2, 6000, 516, 2, "fp32", "gelu", 0.3, True), (1, 3001, 1192, 2, "bf16", "none", 0.7, True),
+    (1, 1500, 2600, 1, "bf16", "silu", 0.5, True), (2, 4100, 24, 1, "fp32", "silu", 0.9, False), (1, 9000, 7, 7, "fp32", "gelu", 0.5, True),
+    (1, 5000, 3, 1, "bf16", "silu", 0.5, True), (2, 700, 1602, 2, "fp32", "silu", 0.5, True), (1, 20000, 64, 32, "bf16", "gelu", 0.99, True)])
+def test_group_norm_with_runs_and_scattered_masked_positions(torch, s2d, N, P, C, G, dtype, act, share, affine):
+    """Many positions of which a run and scattered ones are masked: NaN there, in place and not."""
+    rng = np.random.default_rng(P + C)
+    x, dy = rows(torch, rng, (N, P, C), dtype, 1.5), rows(torch, rng, (N, P, C), dtype)
+    gamma, beta = (torch.from_numpy(v.astype(np.float32)).cuda() if affine else None
+                   for v in (rng.normal(size=C) * 0.3 + 1, rng.normal(size=C) * 0.3))
+    mask = (rng.random((N, P)) < share).astype(np.uint8)
+    mask[0, P // 3:P // 3 + P // 4] = 255
+    mask[-1, -3:] = [0, 1, 0]
+    m = torch.from_numpy(mask).cuda()
+    x[m != 0], dy[m != 0] = float("nan"), float("inf")
+    code = {"none": s2d.ACT_NONE, "silu": s2d.ACT_SILU, "gelu": s2d.ACT_GELU}[act]
+    param = lambda t: None if t is None else host(t)
+    ref = seq.group_norm(host(x), param(gamma), param(beta), G, 1e-5, act, mask, host(dy))
+    y, stats = s2d.group_norm_fwd(x, gamma, beta, G, act=code, mask=m)
+    dx, dgamma, dbeta = s2d.group_norm_bwd(x, gamma, beta, G, stats, dy, act=code, mask=m)
+    for name, got in dict(y=y, dx=dx).items():
+        close(name, got, ref[name], dtype)
+        assert bool((got[m != 0] == 0).all())
+    close("stats", stats, ref["stats"], "fp32")
+    if affine:
+        close("dgamma", dgamma, ref["dgamma"], "fp32")
+        close("dbeta", dbeta, ref["dbeta"], "fp32")
+    assert torch.equal(s2d.group_norm_bwd(x, gamma, beta, G, stats, dy, act=code, mask=m, dx=dy)[0], dx)
+    assert torch.equal(s2d.group_norm_fwd(x, gamma, beta, G, act=code, mask=m, y=x)[0], y)
