@@ -16,7 +16,7 @@
 // The backward pass is the same scan from the last row to the first for e_t = a_t (dh_t + e_{t+1}); it rebuilds the states from the ones in front of each chunk, which the forward saved.
 //
 // Measured (a copy reaches 5.2 TB/s): 65536 x 2048 bf16 forward 255 us, 4.2 TB/s of its bytes; 16384 x 2048 bf16 forward 71 us, 3.8, backward
-// 136 us, 3.5; 5003 x 771 fp32 21 and 39 us; 37 x 256 bf16 6 and 11.5 us, one chunk's latency; clearing the workspace 2 us of each, the sum
+// 136 us, 3.5; 5003 x 771 fp32 21 and 39 us; 37 x 256 bf16 6 and 11 us, one chunk's latency; clearing the workspace 2 us of each, the sum
 // for dlam 4 of the backward.
 //
 // No wait without an end: a workgroup draws its chunk from its column's counter, so every chunk with a smaller number belongs to
@@ -452,6 +452,13 @@ __device__ __forceinline__ void add_row(const RecurArgs& p, const RowBits& bits,
     }
 }
 
+// the map of a wavefront whose rows are of no sequence, which does nothing else (4 x 395 bf16 forward 6.8 us without, 6.0 with; backward 11.6 and 10.9)
+template <int V>
+__device__ __forceinline__ void no_rows(float* A) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) A[v] = kCut;
+}
+
 // ---- forward
 template <int V, int TW, bool PLAIN>
 __device__ __forceinline__ void add_rows(const RecurArgs& p, const RowBits& bits, int c, const float (*a)[V], float (*u)[V], float* A, float* S,
@@ -513,7 +520,8 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
             u[j][v] = g.b * g.si * get<T, V>(xr[j], v);
         }
     if (bits.plain) add_rows<V, TW, true>(p, bits, c, a, u, A, S, h0);
-    else add_rows<V, TW, false>(p, bits, c, a, u, A, S, h0);
+    else if (bits.inside != 0) add_rows<V, TW, false>(p, bits, c, a, u, A, S, h0);
+    else no_rows<V>(A);
 #pragma unroll
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; }
     __syncthreads();
@@ -538,7 +546,7 @@ __global__ __launch_bounds__(64 * NW) void recur_fwd_kernel(const RecurArgs p, i
     }
     const RowPointer ph(p.h, p.sh, EB, t0, p.T);
     if (bits.plain) fwd_rows<T, V, TW, true>(p, bits, c, off, ph, a, u, h);
-    else fwd_rows<T, V, TW, false>(p, bits, c, off, ph, a, u, h);
+    else if (bits.inside != 0) fwd_rows<T, V, TW, false>(p, bits, c, off, ph, a, u, h);
     if (p.hT) pass_empty<V>(p, p.h0, p.hT, c, (long long)k * NW + wave, (long long)chunks * NW);
 }
 
@@ -666,7 +674,8 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
             rows.u[j][v] = g.b * g.si * get<T, V>(rows.x[j], v);
         }
     if (bits.plain) bwd_maps<T, V, TW, true>(p, bits, c, rows, A, S, D, h0, dhT);
-    else bwd_maps<T, V, TW, false>(p, bits, c, rows, A, S, D, h0, dhT);
+    else if (bits.inside != 0) bwd_maps<T, V, TW, false>(p, bits, c, rows, A, S, D, h0, dhT);
+    else no_rows<V>(A);
 #pragma unroll
     for (int v = 0; v < V; ++v) { mapA[wave][lane * V + v] = A[v]; mapS[wave][lane * V + v] = S[v]; mapD[wave][lane * V + v] = D[v]; }
     __syncthreads();
@@ -691,7 +700,7 @@ __global__ __launch_bounds__(64 * NW) void recur_bwd_kernel(const RecurArgs p, f
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(mapA[w][lane * V + v], h[v], mapS[w][lane * V + v]);
     if (bits.plain) bwd_rows<T, V, TW, true>(p, bits, t0, c, off, decay, rows, h, e, sum, h0, dhT);
-    else bwd_rows<T, V, TW, false>(p, bits, t0, c, off, decay, rows, h, e, sum, h0, dhT);
+    else if (bits.inside != 0) bwd_rows<T, V, TW, false>(p, bits, t0, c, off, decay, rows, h, e, sum, h0, dhT);
     if (p.dh0) pass_empty<V>(p, p.dhT, p.dh0, c, (long long)k * NW + wave, (long long)chunks * NW);
     __syncthreads();                                        // the maps have been read
 #pragma unroll
