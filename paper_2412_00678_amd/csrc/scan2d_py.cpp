@@ -390,16 +390,16 @@ struct Rows {
         for (int64_t k = 0; k + 1 < n; ++k) rows *= v.size(k);
         p = v.data_ptr();
         if (v.numel() == 0) return;
-        bool fits = C == 1 || v.stride(n - 1) == 1;
+        bool fits = C == 1 || v.stride(n - 1) == 1, seen = false;
         int64_t span = 0;                          // stride of the whole of the dimensions seen so far
         for (int64_t k = n - 2; k >= 0; --k) {
             if (v.size(k) == 1) continue;
-            if (stride == 0) stride = span = v.stride(k);
+            if (!seen) stride = span = v.stride(k);
             else if (v.stride(k) != span) fits = false;
+            seen = true;
             span *= v.size(k);
         }
-        if (stride != 0 && stride < C) fits = false;
-        if (rows > 1 && stride == 0) fits = false;              // one row read for all
+        if (seen && stride < C) fits = false;                   // 0: one row read for all of a dimension
         if (!fits) raise(PyExc_ValueError, std::string(name) + " must have its channels next to each other and its rows at one stride");
     }
 };
@@ -415,6 +415,7 @@ struct Seq {
     static const at::Tensor& main(PyObject* o, const char* name, int least) {
         const at::Tensor& v = tensor(o, name);
         if (v.dim() < least) raise(PyExc_ValueError, std::string(name) + ": expected at least " + std::to_string(least) + " dimensions, got " + std::to_string(v.dim()));
+        Rows(v, name);                             // its layout, wherever it is
         if (!v.is_cuda()) raise(PyExc_ValueError, std::string(name) + " must be a device tensor");
         if (v.scalar_type() != at::kFloat && v.scalar_type() != at::kBFloat16)
             raise(PyExc_TypeError, std::string(name) + " must be float32 or bfloat16, got " + describe(v.scalar_type(), {}).substr(0, describe(v.scalar_type(), {}).size() - 3));

@@ -193,3 +193,41 @@ def test_binding_refuses_host_tensors(lib):
         lib.group_norm_fwd(torch.zeros(2, 4, 8), None, None, 2)
     with pytest.raises(TypeError):
         lib.seq_recur_step(None, x, x, lam, torch.zeros(4, 8))
+
+
+def broadcasts(C=8):
+    """Views that have one row for all of a dimension, at each place where such a dimension can stand."""
+    return {"all rows": torch.zeros(1, C).expand(6, C), "inner": torch.zeros(4, 1, C).expand(4, 50, C), "outer": torch.zeros(1, 50, C).expand(4, 50, C),
+            "both": torch.zeros(1, 1, C).expand(4, 50, C), "middle of three": torch.zeros(2, 1, 5, C).expand(2, 3, 5, C),
+            "innermost of three": torch.zeros(2, 3, 1, C).expand(2, 3, 5, C), "two of three": torch.zeros(2, 1, 1, C).expand(2, 3, 5, C),
+            "beside a one": torch.zeros(4, 1, 1, C).expand(4, 50, 1, C)}
+
+
+@pytest.mark.parametrize("which", sorted(broadcasts()))
+def test_binding_refuses_rows_that_are_broadcast(lib, which):
+    """A broadcast dimension has fewer rows in memory than its size says.  Layouts are looked at before devices, so that this
+    shows without one."""
+    x, lam = broadcasts()[which], torch.zeros(8)
+    if x.dim() <= 3:
+        with pytest.raises(ValueError, match="rows at one stride"):
+            lib.seq_recur_fwd(x, x, x, lam)
+        with pytest.raises(ValueError, match="rows at one stride"):
+            lib.seq_recur_bwd(x, x, x, lam, x, None)
+    if x.dim() >= 3:
+        with pytest.raises(ValueError, match="rows at one stride"):
+            lib.group_norm_fwd(x, None, None, 2)
+        with pytest.raises(ValueError, match="rows at one stride"):
+            lib.group_norm_bwd(x, None, None, 2, None, x)
+
+
+def test_binding_takes_the_layouts_of_rows(lib):
+    """Views whose rows lie at one stride get as far as the device."""
+    wide = torch.zeros(4, 50, 24)
+    for x in (wide[..., 8:16], wide[:1, :, :8], wide[:, :1, :8], wide[:1, :1, 16:], torch.zeros(0, 5, 8), torch.zeros(4, 50, 8)[:, ::2].contiguous(),
+              torch.zeros(50, 24)[::2, :8], torch.zeros(1, 1, 8).expand(1, 1, 8), torch.zeros(2, 6, 7, 8).permute(0, 1, 2, 3)):
+        if x.dim() <= 3:
+            with pytest.raises(ValueError, match="device tensor"):
+                lib.seq_recur_fwd(x, x, x, torch.zeros(8))
+        if x.dim() >= 3:
+            with pytest.raises(ValueError, match="device tensor"):
+                lib.group_norm_fwd(x, None, None, 2)

@@ -738,3 +738,32 @@ def test_group_norm_with_runs_and_scattered_masked_positions(torch, s2d, N, P, C
         close("dbeta", dbeta, ref["dbeta"], "fp32")
     assert torch.equal(s2d.group_norm_bwd(x, gamma, beta, G, stats, dy, act=code, mask=m, dx=dy)[0], dx)
     assert torch.equal(s2d.group_norm_fwd(x, gamma, beta, G, act=code, mask=m, y=x)[0], y)
+
+
+@pytest.mark.parametrize("shape,one", [((4, 50, 8), (1,)), ((4, 50, 8), (0,)), ((4, 50, 8), (0, 1)), ((2, 3, 5, 8), (1,)), ((2, 3, 5, 8), (2,)),
+                                       ((2, 3, 5, 8), (1, 2)), ((6, 8), (0,))])
+def test_broadcast_rows_are_refused(torch, s2d, shape, one):
+    """Tensors that have one row for all of a dimension, as each argument in turn, read or written: an error and no call."""
+    x = torch.zeros(shape, device="cuda")
+    lam = torch.zeros(8, device="cuda")
+    flat = torch.zeros([1 if k in one else n for k, n in enumerate(shape)], device="cuda").expand(shape)
+    calls = []
+    if len(shape) <= 3:
+        _, _, saved = s2d.seq_recur_fwd(x, x, x, lam, want_saved=True)
+        calls += [(s2d.seq_recur_fwd, dict(x=x, r=x, i=x, lam=lam, h=torch.zeros_like(x)), ("x", "r", "i", "h")),
+                  (s2d.seq_recur_bwd, dict(x=x, r=x, i=x, lam=lam, dh=x, saved=saved), ("x", "r", "i", "dh"))]
+        for k in range(3):
+            with pytest.raises(ValueError, match="rows at one stride"):
+                s2d.seq_recur_bwd(x, x, x, lam, x, saved, out=tuple(flat if q == k else None for q in range(3)))
+    if len(shape) == 2:
+        calls.append((s2d.seq_recur_step, dict(x=x, r=x, i=x, lam=lam, state=torch.zeros(6, 8, device="cuda"), h=torch.zeros_like(x)), ("x", "r", "i", "h")))
+    if len(shape) >= 3:
+        _, stats = s2d.group_norm_fwd(x, None, None, 2)
+        calls += [(s2d.group_norm_fwd, dict(x=x, gamma=None, beta=None, groups=2, y=torch.zeros_like(x)), ("x", "y")),
+                  (s2d.group_norm_bwd, dict(x=x, gamma=None, beta=None, groups=2, stats=stats, dy=x, dx=torch.zeros_like(x)), ("x", "dy", "dx"))]
+    for fn, kw, names in calls:
+        fn(**kw)
+        for name in names:
+            with pytest.raises(ValueError, match="rows at one stride"):
+                fn(**{**kw, name: flat})
+    torch.cuda.synchronize()
