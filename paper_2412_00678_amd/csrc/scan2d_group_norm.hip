@@ -223,14 +223,21 @@ __device__ __forceinline__ void group_sums(const Geo& q, const Lane<V, ONE>& l, 
     team_sync<WAVE>();
 }
 
-// The rows of a team's item that count.
-template <bool WAVE>
-__device__ __forceinline__ int count_rows(int* cnt, int lt, bool counts, int mine) {
-    if (lt == 0) *cnt = 0;
+// The rows that count of R items of a team, each in a counter of its own (cnts[item][at]): wavefronts read them at different times, so a
+// counter is written again only behind another barrier of the team, which the sums of the items are.
+template <bool WAVE, int R, int N>
+__device__ __forceinline__ void count_rows(int (&cnts)[R][N], int at, int lt, bool counts, const int (&mine)[R], int (&rows)[R]) {
+    if (lt == 0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) cnts[i][at] = 0;
+    }
     team_sync<WAVE>();
-    if (counts && mine != 0) atomicAdd(cnt, mine);
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (counts && mine[i] != 0) atomicAdd(&cnts[i][at], mine[i]);
     team_sync<WAVE>();
-    return *cnt;
+#pragma unroll
+    for (int i = 0; i < R; ++i) rows[i] = cnts[i][at];
 }
 
 template <int V>
@@ -257,7 +264,7 @@ template <typename T, int V, bool ONE, int K, int R, int TH, bool WAVE, int ACT>
 __global__ __launch_bounds__(TH) void group_norm_fwd_kernel(const GroupNormArgs p, const Geo q, int teams) {
     constexpr int GV = Lane<V, ONE>::GV, PER = ONE ? 1 : V;                  // floats of red per lane
     __shared__ float red[R * TH * PER], res[2][R][TH * GV];
-    __shared__ int cnts[WAVE ? TH : 1];
+    __shared__ int cnts[R][WAVE ? TH : 1];
     const int tid = threadIdx.x, lt = WAVE ? tid & (q.ts - 1) : tid, base = tid - lt;
     const int team = WAVE ? (int)((blockIdx.x * (long long)TH + tid) / q.ts) : (int)blockIdx.x;      // teams is a multiple of slabs
     const Lane<V, ONE> l(q, p.C, p.G, team % q.slabs, lt);
@@ -269,7 +276,7 @@ __global__ __launch_bounds__(TH) void group_norm_fwd_kernel(const GroupNormArgs 
         Pack<T, V> x[R][K];
         bool live[R][K];
         long long item[R], row0[R];
-        int rows[R];
+        int rows[R], mine[R];
         bool real[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -277,18 +284,18 @@ __global__ __launch_bounds__(TH) void group_norm_fwd_kernel(const GroupNormArgs 
             real[i] = n < p.N && team < teams;              // the last workgroup may have lanes to spare
             item[i] = n;
             row0[i] = (real[i] ? n : 0) * p.P;
-            int mine = 0;
+            mine[i] = 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int r = l.slot + k * q.slots;
                 const long long row = row0[i] + min(r, p.P - 1);
                 x[i][k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
                 live[i][k] = real[i] && l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
-                mine += live[i][k];
+                mine[i] += live[i][k];
             }
             rows[i] = p.P;
-            if (p.mask != nullptr) rows[i] = count_rows<WAVE>(&cnts[base], lt, lt % q.lanes == 0, mine);
         }
+        if (p.mask != nullptr) count_rows<WAVE, R>(cnts, WAVE ? base : 0, lt, lt % q.lanes == 0, mine, rows);
         float s[R][V], mean[R][GV], rstd[R][GV];
 #pragma unroll
         for (int i = 0; i < R; ++i)
@@ -381,7 +388,7 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
     constexpr int GV = Lane<V, ONE>::GV, PER = ONE ? 1 : V;
     constexpr int RED = 2 * R * TH * PER > 2 * TH * V ? 2 * R * TH * PER : 2 * TH * V;       // the channels' sums at the end use it too
     __shared__ float red[RED], res[2][R][TH * GV];
-    __shared__ int cnts[WAVE ? TH : 1];
+    __shared__ int cnts[R][WAVE ? TH : 1];
     const int tid = threadIdx.x, lt = WAVE ? tid & (q.ts - 1) : tid, base = tid - lt;
     const int team = WAVE ? (int)((blockIdx.x * (long long)TH + tid) / q.ts) : (int)blockIdx.x;
     const Lane<V, ONE> l(q, p.C, p.G, team % q.slabs, lt);
@@ -395,14 +402,14 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
         Pack<T, V> x[R][K], dy[R][K];
         bool live[R][K], real[R];
         long long row0[R];
-        int rows[R];
+        int rows[R], mine[R];
         float mean[R][GV], rstd[R][GV];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const long long n = team / q.slabs + ((long long)it * R + i) * step;
             real[i] = n < p.N && team < teams;
             row0[i] = (real[i] ? n : 0) * p.P;
-            int mine = 0;
+            mine[i] = 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int r = l.slot + k * q.slots;
@@ -410,7 +417,7 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
                 x[i][k] = load_pack<T, V>(static_cast<const T*>(p.x) + row * p.sx + l.c);
                 dy[i][k] = load_pack<T, V>(static_cast<const T*>(p.dy) + row * p.sdy + l.c);
                 live[i][k] = real[i] && l.on && r < p.P && (p.mask == nullptr || p.mask[row] == 0);
-                mine += live[i][k];
+                mine[i] += live[i][k];
             }
 #pragma unroll
             for (int v = 0; v < GV; ++v) {
@@ -419,8 +426,8 @@ __global__ __launch_bounds__(TH) void group_norm_bwd_kernel(const GroupNormArgs 
                 rstd[i][v] = st[1];
             }
             rows[i] = p.P;
-            if (p.mask != nullptr) rows[i] = count_rows<WAVE>(&cnts[base], lt, lt % q.lanes == 0, mine);
         }
+        if (p.mask != nullptr) count_rows<WAVE, R>(cnts, WAVE ? base : 0, lt, lt % q.lanes == 0, mine, rows);
         float s[2 * R][V], dv[R][K][V];
 #pragma unroll
         for (int i = 0; i < R; ++i)
@@ -799,14 +806,14 @@ template <typename T, int V, bool ONE, bool MASK>
 __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float4* part) {
     constexpr int PER = ONE ? 1 : V;
     __shared__ float red[kTileThreads * PER], mean_of[kTileThreads * Lane<V, ONE>::GV];
-    __shared__ int cnt;
+    __shared__ int cnt[1][1];
     const Tile t(q, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
     float mean[V], m2[V], n = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) mean[v] = m2[v] = 0.0f;
-    int mine = 0;
+    int mine[1] = {0};
     const int batch = q.slots * kRows;
     Rows<MASK> rows_at;
     const bool (&live)[kRows] = rows_at.live;
@@ -819,7 +826,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const Gr
         int here = 0;
 #pragma unroll
         for (int k = 0; k < kRows; ++k) here += live[k];
-        mine += here;
+        mine[0] += here;
         const float m = (float)here, inv = here > 0 ? 1.0f / m : 0.0f, share = here > 0 ? m / (n + m) : 0.0f, both = n * share;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -838,7 +845,9 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const Gr
         }
         n += m;
     }
-    const int rows = MASK ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
+    int counted[1] = {t.r1 - t.r0};
+    if (MASK) count_rows<false, 1>(cnt, 0, l.lt, l.lt % q.lanes == 0, mine, counted);
+    const int rows = counted[0];
     const float M = (float)rows * (float)l.D, inv = rows > 0 ? 1.0f / M : 0.0f;
     float s[1][V];
 #pragma unroll
@@ -939,7 +948,7 @@ template <typename T, int V, bool ONE, bool MASK, int ACT>
 __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float2* sums, float* counts) {
     constexpr int GV = Lane<V, ONE>::GV;
     __shared__ float red[2][kTileThreads * V];
-    __shared__ int cnt;
+    __shared__ int cnt[1][1];
     const Tile t(q, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
@@ -965,12 +974,12 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) b[v] = g[v] = 0.0f;
-    int mine = 0;
+    int mine[1] = {0};
     for (int r = t.r0; r < t.r1; r += batch) {
         if (r > t.r0) load(r);
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
-            mine += live[k];
+            mine[0] += live[k];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float xh = (get<T, V>(x[k], v) - mean[ONE ? 0 : v]) * rstd[ONE ? 0 : v];
@@ -986,7 +995,9 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const Gro
             red[0][l.slot * l.width + l.c + v - l.lo] = b[v];
             red[1][l.slot * l.width + l.c + v - l.lo] = g[v];
         }
-    const int rows = MASK ? count_rows<false>(&cnt, l.lt, l.lt % q.lanes == 0, mine) : t.r1 - t.r0;
+    int counted[1] = {t.r1 - t.r0};
+    if (MASK) count_rows<false, 1>(cnt, 0, l.lt, l.lt % q.lanes == 0, mine, counted);
+    const int rows = counted[0];
     __syncthreads();
     for (int c = l.lt; c < l.width; c += kTileThreads) {
         float sb = 0.0f, sg = 0.0f;

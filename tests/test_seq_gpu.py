@@ -767,3 +767,14 @@ def test_broadcast_rows_are_refused(torch, s2d, shape, one):
             with pytest.raises(ValueError, match="rows at one stride"):
                 fn(**{**kw, name: flat})
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("N,P,C,G,dtype,act", [
+    # more items than workgroups: each takes several at once.  Groups in a workgroup's slab, many and one, rows that fill it and do not
+    (4100, 9, 192, 32, "bf16", "silu"), (4100, 3, 512, 1, "fp32", "gelu"), (2500, 10, 160, 32, "fp32", "none"), (4099, 4, 512, 1, "bf16", "silu"),
+    (5000, 2, 1024, 2, "bf16", "silu"), (2049, 6, 320, 1, "fp32", "silu"), (2300, 12, 160, 5, "bf16", "gelu"),
+    # teams within a wavefront, and workgroups that take one item after the other
+    (9000, 4, 64, 4, "bf16", "silu"), (40000, 3, 20, 5, "fp32", "silu"), (8200, 2, 516, 3, "bf16", "none"), (2100, 70, 160, 4, "bf16", "silu")])
+def test_group_norm_of_many_masked_items_of_a_few_positions(torch, s2d, N, P, C, G, dtype, act):
+    """Windows with masked positions, different numbers of them, many more than there are workgroups."""
+    norm_case(torch, s2d, N, P, C, G, dtype, act, True, True, seed=N + C)
