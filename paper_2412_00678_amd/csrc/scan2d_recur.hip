@@ -426,7 +426,7 @@ struct Ahead {
         return j == row0 ? a : b;
     }
 };
-// a row's map on top of (A, S); `plain`: known to be neither a first row nor one of no sequence
+// A row's map on top of (A, S); PLAIN: known to be neither a first row nor one of no sequence.  A is the product of the other rows' decays.
 template <bool PLAIN, int V>
 __device__ __forceinline__ void add_row(const RecurArgs& p, const RowBits& bits, int j, int c, const float* a, float* u, float* A, float* S,
                                         const Ahead<V> h0) {
@@ -436,13 +436,10 @@ __device__ __forceinline__ void add_row(const RecurArgs& p, const RowBits& bits,
             for (int v = 0; v < V; ++v) u[v] = fmaf(a[v], h0.get(p, bits, j, c, v), u[v]);
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            S[v] = u[v];
-            A[v] = kCut;
-        }
+        for (int v = 0; v < V; ++v) S[v] = u[v];
     } else if (!PLAIN && !bit(bits.inside, j)) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) { u[v] = S[v] = 0.0f; A[v] = kCut; }
+        for (int v = 0; v < V; ++v) u[v] = S[v] = 0.0f;
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -465,6 +462,12 @@ __device__ __forceinline__ void add_rows(const RecurArgs& p, const RowBits& bits
                                          const Ahead<V> h0) {
 #pragma unroll
     for (int j = 0; j < TW; ++j) add_row<PLAIN, V>(p, bits, j, c, a[j], u[j], A, S, h0);
+    // Rows that hold a first one or one of no sequence forget what comes before them, whatever the decays behind are: a product with a NaN
+    // among them would not, and the backward pass would carry it to the sequence in front.
+    if (!PLAIN && ((bits.first | ~bits.inside) & ((1ull << TW) - 1)) != 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = kCut;
+    }
 }
 template <typename T, int V, int TW, bool PLAIN>
 __device__ __forceinline__ void fwd_rows(const RecurArgs& p, const RowBits& bits, int c, uint32_t off, const RowPointer row, const float (*a)[V],

@@ -778,3 +778,49 @@ def test_broadcast_rows_are_refused(torch, s2d, shape, one):
 def test_group_norm_of_many_masked_items_of_a_few_positions(torch, s2d, N, P, C, G, dtype, act):
     """Windows with masked positions, different numbers of them, many more than there are workgroups."""
     norm_case(torch, s2d, N, P, C, G, dtype, act, True, True, seed=N + C)
+
+
+@pytest.mark.parametrize("where", ["r", "-r", "i", "x", "dh", "h0", "dhT"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("lens", [(16, 19, 40, 8), (50, 3, 160, 20, 1, 64), (1000, 608, 3, 996, 1403, 700)], ids=["one chunk", "chunks", "groups of chunks"])
+def test_recurrence_nan_stays_in_its_sequence_forward_and_backward(torch, s2d, lens, dtype, where):
+    """A NaN of either sign in one sequence, one to seven rows behind its first in different channels (among the rows of one
+    wavefront, that is): the other sequences keep their bits in every output, and a channel without one keeps all of them."""
+    rng = np.random.default_rng(len(lens))
+    T, S, C = sum(lens), len(lens), 72
+    ends = np.cumsum(lens)
+    off = torch.tensor([0, *ends], dtype=torch.int32, device="cuda")
+    lam = torch.from_numpy(decays(rng, C)).cuda()
+    x, r, i, dh = (rows(torch, rng, (T, C), dtype) for _ in range(4))
+    h0, dhT = (torch.from_numpy(rng.normal(size=(S, C)).astype(np.float32)).cuda() for _ in range(2))
+
+    def once(x, r, i, dh, h0, dhT):
+        h, hT, saved = s2d.seq_recur_fwd(x, r, i, lam, offsets=off, h0=h0, want_final=True, want_saved=True)
+        dx, dr, di, dlam, dh0 = s2d.seq_recur_bwd(x, r, i, lam, dh, saved, offsets=off, h0=h0, dhT=dhT)
+        torch.cuda.synchronize()
+        return dict(h=h, dx=dx, dr=dr, di=di), dict(hT=hT, dh0=dh0), dlam
+
+    clean = once(x, r, i, dh, h0, dhT)
+    channels = torch.arange(1, C, device="cuda")                               # channel 0 has none
+    for s in range(S):
+        v = dict(x=x, r=r, i=i, dh=dh, h0=h0, dhT=dhT)
+        name = where[-1] if where[0] == "-" else where
+        t = v[name] = v[name].clone()
+        nan = torch.tensor(float("nan"), device="cuda").to(t.dtype)
+        nan = torch.copysign(nan, torch.tensor(-1.0 if where[0] == "-" else 1.0, device="cuda").to(t.dtype))
+        if name in ("h0", "dhT"):
+            t[s, 1:] = nan
+        else:
+            at = torch.clamp(int(ends[s]) - lens[s] + 1 + channels % 7, max=int(ends[s]) - 1)
+            t[at, channels] = nan
+        got = once(**v)
+        others = torch.ones(T, dtype=torch.bool, device="cuda")
+        others[int(ends[s]) - lens[s]:int(ends[s])] = False
+        rest = [k for k in range(S) if k != s]
+        for n in clean[0]:
+            assert torch.equal(got[0][n][others], clean[0][n][others]), (n, s)
+            assert torch.equal(got[0][n][:, 0], clean[0][n][:, 0]), (n, s)
+        for n in clean[1]:
+            assert torch.equal(got[1][n][rest], clean[1][n][rest]), (n, s)
+            assert torch.equal(got[1][n][:, 0], clean[1][n][:, 0]), (n, s)
+        assert torch.equal(got[2][:1], clean[2][:1]), s
