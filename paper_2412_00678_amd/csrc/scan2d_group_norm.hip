@@ -1021,12 +1021,12 @@ __device__ __forceinline__ float block_rows(const float* counts, size_t n, int c
     for (int k = 0; k < kJoinThreads / 64; ++k) rows += rows_of[k];
     return rows;
 }
-__global__ __launch_bounds__(kJoinThreads) void group_norm_chan_kernel(const float2* sums, const float* counts, int chunks, int C, int G, int D, int gw,
+__global__ __launch_bounds__(kJoinThreads) void group_norm_chan_kernel(const float2* sums, const float* counts, int chunks, int n0, int C, int G, int D, int gw,
                                                                        const float* gamma, float2* chan, float2* coef, float* dgamma, float* dbeta) {
     __shared__ float2 red[kJoinThreads], total[kJoinThreads];
     __shared__ float rows_of[kJoinThreads / 64];
     const int tid = threadIdx.x, sets = (G + gw - 1) / gw, g0 = (blockIdx.x % sets) * gw;
-    const size_t n = blockIdx.x / sets;
+    const size_t n = n0 + blockIdx.x / sets;
     const int groups = min(gw, G - g0), w = groups * D, lo = g0 * D, shares = kJoinThreads / w, c = tid % w, share = tid / w;
     float2 s = make_float2(0.0f, 0.0f);
     if (share < shares) {
@@ -1055,10 +1055,10 @@ __global__ __launch_bounds__(kJoinThreads) void group_norm_chan_kernel(const flo
     }
 }
 // Wider groups: 16 channels of an item per workgroup, then one workgroup per item and group.
-__global__ __launch_bounds__(kJoinThreads) void group_norm_wide_chan_kernel(const float2* sums, int chunks, int C, float2* chan, float* dgamma, float* dbeta) {
+__global__ __launch_bounds__(kJoinThreads) void group_norm_wide_chan_kernel(const float2* sums, int chunks, int n0, int C, float2* chan, float* dgamma, float* dbeta) {
     __shared__ float2 red[64][16];
     const int cols = (C + 15) / 16, lane = threadIdx.x & 15, share = threadIdx.x >> 4, c = (blockIdx.x % cols) * 16 + lane;
-    const size_t n = blockIdx.x / cols;
+    const size_t n = n0 + blockIdx.x / cols;
     float2 s = make_float2(0.0f, 0.0f);
     if (c < C) {
 #pragma unroll 8
@@ -1076,12 +1076,12 @@ __global__ __launch_bounds__(kJoinThreads) void group_norm_wide_chan_kernel(cons
         if (dgamma) dgamma[c] = s.y;
     }
 }
-__global__ __launch_bounds__(kJoinThreads) void group_norm_wide_coef_kernel(const float2* chan, const float* counts, int chunks, int G, int D, const float* gamma,
+__global__ __launch_bounds__(kJoinThreads) void group_norm_wide_coef_kernel(const float2* chan, const float* counts, int chunks, int n0, int G, int D, const float* gamma,
                                                                             float2* coef) {
     __shared__ float2 red[kJoinThreads / 64];
     __shared__ float rows_of[kJoinThreads / 64];
     const int tid = threadIdx.x, g = blockIdx.x % G;
-    const size_t n = blockIdx.x / G;
+    const size_t n = n0 + blockIdx.x / G;
     float2 t = make_float2(0.0f, 0.0f);
     for (int d = tid; d < D; d += kJoinThreads) {
         const float2 c = chan[(n * G + g) * D + d];
@@ -1281,6 +1281,14 @@ NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
 bool join_in_apply(const NormPlan& n) { return (long long)n.chunks * n.q.spg * n.q.gps <= 2048; }
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 int launched() { return hipGetLastError() == hipSuccess ? SCAN2D_OK : SCAN2D_ERR_LAUNCH_FAILED; }
+// `each` workgroups for each of N items, in as many launches as it takes to stay below 2^32 threads in one: launch(first item, workgroups).
+// (16384 tokens of 4096 channels in one group, 16 channels a workgroup of 1024, are two.  Workgroups that go on to further items
+// instead cost shapes of any size: 32 x 3136 x 192 backward 43.8 -> 46.3 us.)
+template <typename Launch>
+void by_items(int N, long long each, int threads, Launch launch) {
+    const long long most = ((1LL << 32) - 1) / (threads * each);
+    for (long long n = 0; n < N; n += most) launch((int)n, dim3((unsigned)((N - n < most ? N - n : most) * each)));
+}
 
 template <typename T, int V, bool ONE, int ACT>
 int fwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
@@ -1300,9 +1308,9 @@ int fwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
 template <typename T, int V, bool ONE, int ACT, bool MASK>
 int fwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const long long blocks = (long long)a.N * n.chunks * n.q.slabs, groups = (long long)a.N * a.G;
-    if (!launch_fits(blocks, kTileThreads) || !launch_fits(groups, 64)) return SCAN2D_ERR_BAD_SHAPE;
-    float4* part = static_cast<float4*>(a.workspace);
     const bool in_apply = join_in_apply(n);
+    if (!launch_fits(blocks, kTileThreads) || (!in_apply && !launch_fits(groups, 64))) return SCAN2D_ERR_BAD_SHAPE;
+    float4* part = static_cast<float4*>(a.workspace);
     hipLaunchKernelGGL((group_norm_tiles_kernel<T, V, ONE, MASK>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, part);
     if (!in_apply)
         hipLaunchKernelGGL(group_norm_join_kernel, dim3((unsigned)groups), dim3(64), 0, stream, part, n.chunks * n.q.spg, a.eps, a.stats);
@@ -1333,8 +1341,8 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const unsigned cols = (a.C + 15) / 16;
     const bool narrow = a.D <= kNarrow;
     const int gw = a.D >= 16 ? 1 : (16 + a.D - 1) / a.D, sets = (a.G + gw - 1) / gw;
-    const long long blocks = (long long)a.N * n.chunks * n.q.slabs, joins = (long long)a.N * (narrow ? sets : cols), groups = (long long)a.N * a.G;
-    if (!launch_fits(blocks + cols, kTileThreads) || !launch_fits(joins, kJoinThreads) || !launch_fits(groups, kJoinThreads)) return SCAN2D_ERR_BAD_SHAPE;
+    const long long blocks = (long long)a.N * n.chunks * n.q.slabs;
+    if (!launch_fits(blocks + cols, kTileThreads)) return SCAN2D_ERR_BAD_SHAPE;
     char* w = static_cast<char*>(a.workspace);
     const size_t items = (size_t)a.N * n.chunks;
     float2* sums = reinterpret_cast<float2*>(w);
@@ -1348,11 +1356,17 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     hipLaunchKernelGGL((group_norm_sums_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, sums, counts);
     float *const dgamma = several ? nullptr : a.dgamma, *const dbeta = several ? nullptr : a.dbeta;
     if (narrow) {
-        hipLaunchKernelGGL(group_norm_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, a.C, a.G, a.D, gw, a.gamma,
-                           several ? chan : nullptr, coef, dgamma, dbeta);
+        by_items(a.N, sets, kJoinThreads, [&](int n0, dim3 wgs) {
+            hipLaunchKernelGGL(group_norm_chan_kernel, wgs, dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, n0, a.C, a.G, a.D, gw, a.gamma,
+                               several ? chan : nullptr, coef, dgamma, dbeta);
+        });
     } else {
-        hipLaunchKernelGGL(group_norm_wide_chan_kernel, dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, sums, n.chunks, a.C, chan, dgamma, dbeta);
-        hipLaunchKernelGGL(group_norm_wide_coef_kernel, dim3((unsigned)groups), dim3(kJoinThreads), 0, stream, chan, counts, n.chunks, a.G, a.D, a.gamma, coef);
+        by_items(a.N, cols, kJoinThreads, [&](int n0, dim3 wgs) {
+            hipLaunchKernelGGL(group_norm_wide_chan_kernel, wgs, dim3(kJoinThreads), 0, stream, sums, n.chunks, n0, a.C, chan, dgamma, dbeta);
+        });
+        by_items(a.N, a.G, kJoinThreads, [&](int n0, dim3 wgs) {
+            hipLaunchKernelGGL(group_norm_wide_coef_kernel, wgs, dim3(kJoinThreads), 0, stream, chan, counts, n.chunks, n0, a.G, a.D, a.gamma, coef);
+        });
     }
     hipLaunchKernelGGL((group_norm_grad_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks + (several ? cols : 0)), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, coef,
                        (unsigned)blocks, chan);

@@ -824,3 +824,33 @@ def test_recurrence_nan_stays_in_its_sequence_forward_and_backward(torch, s2d, l
             assert torch.equal(got[1][n][rest], clean[1][n][rest]), (n, s)
             assert torch.equal(got[1][n][:, 0], clean[1][n][:, 0]), (n, s)
         assert torch.equal(got[2][:1], clean[2][:1]), s
+
+
+@pytest.mark.parametrize("N,P,C,G", [(16384, 1, 4096, 1), (16384, 520, 256, 256), (5000, 81, 320, 1)])
+def test_group_norm_backward_of_many_items(torch, s2d, N, P, C, G):
+    """As many items and channels as would need 2^32 threads in one launch of the kernels that join the items' sums (and fewer): the first and
+    last items, and the parameters' sums of some channels, against the oracle."""
+    g = torch.Generator(device="cuda").manual_seed(N + C)
+    make = lambda: torch.empty((N, P, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    x, dy = make(), make()
+    rng = np.random.default_rng(N)
+    gamma, beta = (torch.from_numpy((rng.normal(size=C) * 0.2 + m).astype(np.float32)).cuda() for m in (1.0, 0.0))
+    print(f"group norm backward N={N} P={P} C={C} G={G}", flush=True)
+    y, stats = s2d.group_norm_fwd(x, gamma, beta, G)
+    dx, dgamma, dbeta = s2d.group_norm_bwd(x, gamma, beta, G, stats, dy)
+    torch.cuda.synchronize()
+    for part in (slice(0, 3), slice(N // 2, N // 2 + 3), slice(N - 3, N)):
+        ref = seq.group_norm(host(x[part]), host(gamma), host(beta), G, 1e-5, dy=host(dy[part]))
+        for name, got in (("y", y), ("dx", dx)):
+            close(name, got[part], ref[name], "bf16")
+        close("stats", stats[part], ref["stats"], "fp32")
+    # dbeta = sum dy, dgamma = sum dy xh: a sum over N P terms in at least 32 partial sums of which up to 72 are joined (the oracle's
+    # count), and xh from the statistics with 4 roundings
+    U = 2.0 ** -24
+    for c in (0, 1, C // 2, C - 1):
+        d, v = dy[:, :, c].double(), x[:, :, c].double()
+        m, rs = (stats[:, c // (C // G), k].double()[:, None] for k in (0, 1))
+        terms = d * (v - m) * rs
+        slack = (N * P / 32 + 72) * U
+        assert abs(float(dbeta[c]) - float(d.sum())) <= slack * float(d.abs().sum()), c
+        assert abs(float(dgamma[c]) - float(terms.sum())) <= (slack + 4 * U) * float((d.abs() * (v.abs() + m.abs()) * rs).sum()), c
