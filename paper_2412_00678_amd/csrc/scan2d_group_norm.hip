@@ -758,11 +758,11 @@ constexpr int kTileThreads = 512, kRows = 4;
 struct Tile {
     long long n;
     int chunk, slab, r0, r1;             // the tile's positions
-    __device__ Tile(const Geo& q, int chunks, int per, int P) {
+    __device__ Tile(const Geo& q, int n0, int chunks, int per, int P) {
         slab = blockIdx.x % q.slabs;
         const unsigned r = blockIdx.x / q.slabs;
         chunk = r % chunks;
-        n = r / chunks;
+        n = n0 + (int)(r / chunks);
         r0 = chunk * per;
         r1 = P - r0 < per ? P : r0 + per;                   // r0 + per may pass 2^31
     }
@@ -803,11 +803,11 @@ struct Rows {
 
 // part[(n G + g) E + e] = (values, mean, squared deviations), E = chunks x spg tiles of a group
 template <typename T, int V, bool ONE, bool MASK>
-__global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float4* part) {
+__global__ __launch_bounds__(kTileThreads) void group_norm_tiles_kernel(const GroupNormArgs p, const Geo q, int n0, int chunks, int per, float4* part) {
     constexpr int PER = ONE ? 1 : V;
     __shared__ float red[kTileThreads * PER], mean_of[kTileThreads * Lane<V, ONE>::GV];
     __shared__ int cnt[1][1];
-    const Tile t(q, chunks, per, p.P);
+    const Tile t(q, n0, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
     float mean[V], m2[V], n = 0.0f;
@@ -888,10 +888,10 @@ __global__ __launch_bounds__(64) void group_norm_join_kernel(const float4* part,
 
 // part: the tiles, to be joined here, or null: the statistics are there.
 template <typename T, int V, bool ONE, bool MASK, int ACT>
-__global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, const float4* part) {
+__global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const GroupNormArgs p, const Geo q, int n0, int chunks, int per, const float4* part) {
     constexpr int GV = Lane<V, ONE>::GV;
     __shared__ float2 joined[kTileThreads * GV];
-    const Tile t(q, chunks, per, p.P);
+    const Tile t(q, n0, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
     const int batch = q.slots * kRows, last = t.r0 + (t.r1 - 1 - t.r0) / batch * batch;
@@ -945,11 +945,11 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_apply_kernel(const Gr
 
 // sums[n][chunk][C] = (sum dv, sum dv xh) of a tile; counts[n][chunk]: its rows that count
 template <typename T, int V, bool ONE, bool MASK, int ACT>
-__global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, float2* sums, float* counts) {
+__global__ __launch_bounds__(kTileThreads) void group_norm_sums_kernel(const GroupNormArgs p, const Geo q, int n0, int chunks, int per, float2* sums, float* counts) {
     constexpr int GV = Lane<V, ONE>::GV;
     __shared__ float red[2][kTileThreads * V];
     __shared__ int cnt[1][1];
-    const Tile t(q, chunks, per, p.P);
+    const Tile t(q, n0, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     const long long row0 = t.n * p.P;
     const int batch = q.slots * kRows;
@@ -1102,7 +1102,7 @@ __global__ __launch_bounds__(kJoinThreads) void group_norm_wide_coef_kernel(cons
 
 // The workgroups behind the tiles' join the items' sums to dbeta and dgamma.
 template <typename T, int V, bool ONE, bool MASK, int ACT>
-__global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const GroupNormArgs p, const Geo q, int chunks, int per, const float2* coef, unsigned tiles,
+__global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const GroupNormArgs p, const Geo q, int n0, int chunks, int per, const float2* coef, unsigned tiles,
                                                                        const float2* chan) {
     constexpr int GV = Lane<V, ONE>::GV;
     __shared__ float2 red[kTileThreads / 16][16];
@@ -1110,7 +1110,7 @@ __global__ __launch_bounds__(kTileThreads) void group_norm_grad_kernel(const Gro
         join_params(chan, p.N, p.C, p.dgamma, p.dbeta, blockIdx.x - tiles, threadIdx.x >> 4, kTileThreads / 16, threadIdx.x & 15, red);
         return;
     }
-    const Tile t(q, chunks, per, p.P);
+    const Tile t(q, n0, chunks, per, p.P);
     const Lane<V, ONE> l(q, p.C, p.G, t.slab, threadIdx.x);
     if (!l.on) return;
     const long long row0 = t.n * p.P;
@@ -1281,13 +1281,13 @@ NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
 bool join_in_apply(const NormPlan& n) { return (long long)n.chunks * n.q.spg * n.q.gps <= 2048; }
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 int launched() { return hipGetLastError() == hipSuccess ? SCAN2D_OK : SCAN2D_ERR_LAUNCH_FAILED; }
-// `each` workgroups for each of N items, in as many launches as it takes to stay below 2^32 threads in one: launch(first item, workgroups).
-// (16384 tokens of 4096 channels in one group, 16 channels a workgroup of 1024, are two.  Workgroups that go on to further items
-// instead cost shapes of any size: 32 x 3136 x 192 backward 43.8 -> 46.3 us.)
+// `each` workgroups for each of N items: launch(first item, workgroups) for as many items at a time as stay below 2^31 threads, half of what a
+// launch may hold, so that the gradient's further workgroups fit beside them.  (16384 tokens of 4096 channels in one group are joined by 2^32
+// threads.  Workgroups that go on to further items instead cost shapes of any size: 32 x 3136 x 192 backward 43.8 -> 46.3 us.)
 template <typename Launch>
-void by_items(int N, long long each, int threads, Launch launch) {
-    const long long most = ((1LL << 32) - 1) / (threads * each);
-    for (long long n = 0; n < N; n += most) launch((int)n, dim3((unsigned)((N - n < most ? N - n : most) * each)));
+void by_items(int N, int each, int threads, Launch launch) {
+    const long long most = (1LL << 31) / ((long long)threads * each);
+    for (long long n = 0; n < N; n += most) launch((int)n, (unsigned)((N - n < most ? N - n : most) * each));
 }
 
 template <typename T, int V, bool ONE, int ACT>
@@ -1307,14 +1307,18 @@ int fwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
 }
 template <typename T, int V, bool ONE, int ACT, bool MASK>
 int fwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
-    const long long blocks = (long long)a.N * n.chunks * n.q.slabs, groups = (long long)a.N * a.G;
+    const int each = n.chunks * n.q.slabs;
     const bool in_apply = join_in_apply(n);
-    if (!launch_fits(blocks, kTileThreads) || (!in_apply && !launch_fits(groups, 64))) return SCAN2D_ERR_BAD_SHAPE;
     float4* part = static_cast<float4*>(a.workspace);
-    hipLaunchKernelGGL((group_norm_tiles_kernel<T, V, ONE, MASK>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, part);
-    if (!in_apply)
-        hipLaunchKernelGGL(group_norm_join_kernel, dim3((unsigned)groups), dim3(64), 0, stream, part, n.chunks * n.q.spg, a.eps, a.stats);
-    hipLaunchKernelGGL((group_norm_apply_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, in_apply ? part : nullptr);
+    by_items(a.N, each, kTileThreads, [&](int n0, unsigned wgs) {
+        hipLaunchKernelGGL((group_norm_tiles_kernel<T, V, ONE, MASK>), dim3(wgs), dim3(kTileThreads), 0, stream, a, n.q, n0, n.chunks, n.per, part);
+    });
+    if (!in_apply)                                          // several tiles an item: fewer than 512 slabs in all, of up to 2048 groups each
+        hipLaunchKernelGGL(group_norm_join_kernel, dim3((unsigned)(a.N * a.G)), dim3(64), 0, stream, part, n.chunks * n.q.spg, a.eps, a.stats);
+    by_items(a.N, each, kTileThreads, [&](int n0, unsigned wgs) {
+        hipLaunchKernelGGL((group_norm_apply_kernel<T, V, ONE, MASK, ACT>), dim3(wgs), dim3(kTileThreads), 0, stream, a, n.q, n0, n.chunks, n.per,
+                           in_apply ? part : nullptr);
+    });
     return launched();
 }
 template <typename T, int V, bool ONE, int ACT>
@@ -1340,9 +1344,7 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     const bool params = a.dgamma != nullptr || a.dbeta != nullptr;
     const unsigned cols = (a.C + 15) / 16;
     const bool narrow = a.D <= kNarrow;
-    const int gw = a.D >= 16 ? 1 : (16 + a.D - 1) / a.D, sets = (a.G + gw - 1) / gw;
-    const long long blocks = (long long)a.N * n.chunks * n.q.slabs;
-    if (!launch_fits(blocks + cols, kTileThreads)) return SCAN2D_ERR_BAD_SHAPE;
+    const int gw = a.D >= 16 ? 1 : (16 + a.D - 1) / a.D, sets = (a.G + gw - 1) / gw, each = n.chunks * n.q.slabs;
     char* w = static_cast<char*>(a.workspace);
     const size_t items = (size_t)a.N * n.chunks;
     float2* sums = reinterpret_cast<float2*>(w);
@@ -1353,23 +1355,27 @@ int bwd_split(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     w += up((size_t)a.N * a.C * sizeof(float2));
     float2* coef = reinterpret_cast<float2*>(w);
     const bool several = params && a.N > 1;
-    hipLaunchKernelGGL((group_norm_sums_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, sums, counts);
+    by_items(a.N, each, kTileThreads, [&](int n0, unsigned wgs) {
+        hipLaunchKernelGGL((group_norm_sums_kernel<T, V, ONE, MASK, ACT>), dim3(wgs), dim3(kTileThreads), 0, stream, a, n.q, n0, n.chunks, n.per, sums, counts);
+    });
     float *const dgamma = several ? nullptr : a.dgamma, *const dbeta = several ? nullptr : a.dbeta;
     if (narrow) {
-        by_items(a.N, sets, kJoinThreads, [&](int n0, dim3 wgs) {
-            hipLaunchKernelGGL(group_norm_chan_kernel, wgs, dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, n0, a.C, a.G, a.D, gw, a.gamma,
+        by_items(a.N, sets, kJoinThreads, [&](int n0, unsigned wgs) {
+            hipLaunchKernelGGL(group_norm_chan_kernel, dim3(wgs), dim3(kJoinThreads), 0, stream, sums, counts, n.chunks, n0, a.C, a.G, a.D, gw, a.gamma,
                                several ? chan : nullptr, coef, dgamma, dbeta);
         });
     } else {
-        by_items(a.N, cols, kJoinThreads, [&](int n0, dim3 wgs) {
-            hipLaunchKernelGGL(group_norm_wide_chan_kernel, wgs, dim3(kJoinThreads), 0, stream, sums, n.chunks, n0, a.C, chan, dgamma, dbeta);
+        by_items(a.N, cols, kJoinThreads, [&](int n0, unsigned wgs) {
+            hipLaunchKernelGGL(group_norm_wide_chan_kernel, dim3(wgs), dim3(kJoinThreads), 0, stream, sums, n.chunks, n0, a.C, chan, dgamma, dbeta);
         });
-        by_items(a.N, a.G, kJoinThreads, [&](int n0, dim3 wgs) {
-            hipLaunchKernelGGL(group_norm_wide_coef_kernel, wgs, dim3(kJoinThreads), 0, stream, chan, counts, n.chunks, n0, a.G, a.D, a.gamma, coef);
+        by_items(a.N, a.G, kJoinThreads, [&](int n0, unsigned wgs) {
+            hipLaunchKernelGGL(group_norm_wide_coef_kernel, dim3(wgs), dim3(kJoinThreads), 0, stream, chan, counts, n.chunks, n0, a.G, a.D, a.gamma, coef);
         });
     }
-    hipLaunchKernelGGL((group_norm_grad_kernel<T, V, ONE, MASK, ACT>), dim3((unsigned)blocks + (several ? cols : 0)), dim3(kTileThreads), 0, stream, a, n.q, n.chunks, n.per, coef,
-                       (unsigned)blocks, chan);
+    by_items(a.N, each, kTileThreads, [&](int n0, unsigned wgs) {
+        hipLaunchKernelGGL((group_norm_grad_kernel<T, V, ONE, MASK, ACT>), dim3(wgs + (several && n0 == 0 ? cols : 0)), dim3(kTileThreads), 0, stream, a, n.q, n0,
+                           n.chunks, n.per, coef, wgs, chan);
+    });
     return launched();
 }
 

@@ -826,10 +826,10 @@ def test_recurrence_nan_stays_in_its_sequence_forward_and_backward(torch, s2d, l
         assert torch.equal(got[2][:1], clean[2][:1]), s
 
 
-@pytest.mark.parametrize("N,P,C,G", [(16384, 1, 4096, 1), (16384, 520, 256, 256), (5000, 81, 320, 1)])
+@pytest.mark.parametrize("N,P,C,G", [(16384, 1, 4096, 1), (16384, 520, 256, 256), (5000, 81, 320, 1), (1700001, 1, 2049, 1)])
 def test_group_norm_backward_of_many_items(torch, s2d, N, P, C, G):
-    """As many items and channels as would need 2^32 threads in one launch of the kernels that join the items' sums (and fewer): the first and
-    last items, and the parameters' sums of some channels, against the oracle."""
+    """As many items and channels as would need 2^32 threads in one launch of the kernels that join the items' sums (and fewer), and of the
+    tiles themselves: the first and last items, and the parameters' sums of some channels, against the oracle."""
     g = torch.Generator(device="cuda").manual_seed(N + C)
     make = lambda: torch.empty((N, P, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
     x, dy = make(), make()
