@@ -848,8 +848,12 @@ int clear_chain(const RecurPlan& q, void* workspace, hipStream_t stream) {
     hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, static_cast<uint4*>(workspace), n);
     return launched();
 }
-bool plan_fits(const RecurPlan& q) {
-    return launch_fits((long long)q.chunks * q.cols, 64 * q.waves) && launch_fits((long long)(chain_bytes(q) / 4096 + 1), 256);
+// The chunks in as many launches as it takes to stay below 2^32 threads in each: launch(workgroups).  Each does as many chunks of every column and
+// goes on where the one before left the counters and the states.
+template <typename Launch>
+void by_chunks(const RecurPlan& q, Launch launch) {
+    const long long most = ((1LL << 32) - 1) / (64LL * q.waves * q.cols);
+    for (long long left = q.chunks; left > 0; left -= most) launch((unsigned)((left < most ? left : most) * q.cols));
 }
 
 int launch_none(const RecurArgs& a, const float* from, float* to, float* zero, hipStream_t stream) {
@@ -871,7 +875,6 @@ int recur_fwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
     const RecurPlan q = plan_of(d, SCAN2D_PASS_FWD);
     (void)hipGetLastError();
     if (q.chunks == 0) return a.hT ? launch_none(a, a.h0, a.hT, nullptr, stream) : SCAN2D_OK;
-    if (!plan_fits(q)) return SCAN2D_ERR_BAD_SHAPE;
     if (q.chunks > 1) {
         const int rc = clear_chain(q, a.workspace, stream);
         if (rc != SCAN2D_OK) return rc;
@@ -881,7 +884,7 @@ int recur_fwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
     if (d->dtype != SCAN2D_BF16) k = q.V == 2 ? recur_fwd_kernel<float, 2, 8, kFwdWaves> : q.rows == 8 ? recur_fwd_kernel<float, 1, 8, kFwdWaves> : recur_fwd_kernel<float, 1, 16, kFwdWaves>;
     else if (q.rows == 8) k = q.V == 1 ? recur_fwd_kernel<bf16_t, 1, 8, kFwdWaves> : recur_fwd_kernel<bf16_t, 2, 8, kFwdWaves>;
     else k = q.V == 1 ? recur_fwd_kernel<bf16_t, 1, 16, kFwdWaves> : recur_fwd_kernel<bf16_t, 2, 16, kFwdWaves>;
-    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * q.waves), 0, stream, a, q.chunks, q.cols);
+    by_chunks(q, [&](unsigned wgs) { hipLaunchKernelGGL(k, dim3(wgs), dim3(64 * q.waves), 0, stream, a, q.chunks, q.cols); });
     return launched();
 }
 
@@ -889,7 +892,6 @@ int recur_bwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
     const RecurPlan q = plan_of(d, SCAN2D_PASS_BWD);
     (void)hipGetLastError();
     if (q.chunks == 0) return launch_none(a, a.dhT, a.dh0, a.dlam, stream);
-    if (!plan_fits(q)) return SCAN2D_ERR_BAD_SHAPE;
     float* parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + chain_bytes(q));
     if (q.chunks > 1) {
         const int rc = clear_chain(q, a.workspace, stream);
@@ -898,7 +900,7 @@ int recur_bwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
     using Kernel = void (*)(const RecurArgs, float*, int, int);
     const Kernel k = d->dtype == SCAN2D_BF16 ? (q.V == 1 ? recur_bwd_kernel<bf16_t, 1, kBwdRows, kBwdWaves> : recur_bwd_kernel<bf16_t, 2, kBwdRows, kBwdWaves>)
                                              : (q.V == 1 ? recur_bwd_kernel<float, 1, kBwdRows, kBwdWaves> : recur_bwd_kernel<float, 2, kBwdRows, kBwdWaves>);
-    hipLaunchKernelGGL(k, dim3((unsigned)(q.chunks * q.cols)), dim3(64 * q.waves), 0, stream, a, parts, q.chunks, q.cols);
+    by_chunks(q, [&](unsigned wgs) { hipLaunchKernelGGL(k, dim3(wgs), dim3(64 * q.waves), 0, stream, a, parts, q.chunks, q.cols); });
     if (q.chunks > 1)
         hipLaunchKernelGGL(recur_dlam_kernel, dim3((a.C + 15) / 16), dim3(1024), 0, stream, parts, q.chunks, a.C, a.lam, a.dlam);
     return launched();

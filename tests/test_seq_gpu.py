@@ -854,3 +854,33 @@ def test_group_norm_backward_of_many_items(torch, s2d, N, P, C, G):
         slack = (N * P / 32 + 72) * U
         assert abs(float(dbeta[c]) - float(d.sum())) <= slack * float(d.abs().sum()), c
         assert abs(float(dgamma[c]) - float(terms.sum())) <= (slack + 4 * U) * float((d.abs() * (v.abs() + m.abs()) * rs).sum()), c
+
+
+def test_recurrence_of_as_many_rows_as_there_may_be(torch, s2d):
+    """2^31 - 4097 rows, whose chunks take several launches: rows at both ends and on both sides of every cut against the oracle."""
+    T, C = 2 ** 31 - 4097, 1
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty((T, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    lam = torch.zeros(C, device="cuda")                                        # scale 8: a state is forgotten within some ten tokens
+    print(f"recurrence T={T} C={C}", flush=True)
+    h, hT, saved = s2d.seq_recur_fwd(x, x, x, lam, want_final=True, want_saved=True)
+    torch.cuda.synchronize()
+    dx, dr, di, dlam, _ = s2d.seq_recur_bwd(x, x, x, lam, x, saved)
+    torch.cuda.synchronize()
+    most, chunks = (2 ** 32 - 1) // 768, -(-T // 96)                           # chunks of a launch backward; and below, forward
+    cuts = [8388607 * 128, 2 * 8388607 * 128] + [(chunks - k * most) * 96 for k in range(1, 5)]
+    for lo, hi in [(0, 500), (T - 500, T)] + [(c - 300, c + 300) for c in cuts if 300 <= c <= T - 300]:
+        w = host(x[lo:hi])
+        ref = seq.recur(w, w, w, host(lam), [(0, hi - lo)], dh=w)
+        clear = slice(0 if lo == 0 else 200, hi - lo if hi == T else hi - lo - 200)      # behind 200 rows nothing of a cut is left
+        for name, got in dict(h=h, dx=dx, dr=dr, di=di).items():
+            close(name, got[lo:hi][clear], tuple(t[clear] for t in ref[name]), "bf16")
+        if hi == T:
+            close("hT", hT, ref["hT"], "fp32")
+    # dlam from dr = q (1 - sigmoid(r)), each off by half a step, and the library's sums: a share of the chunks in a row, 64 of these
+    total, size = 0.0, 0.0
+    for lo in range(0, T, 2 ** 28):
+        q = dr[lo:lo + 2 ** 28].double() / torch.sigmoid(-x[lo:lo + 2 ** 28].double())
+        total, size = total + float(q.sum()), size + float(q.abs().sum())
+    ratio = 0.5 / np.log(2.0)                                                  # sigmoid(0) / softplus(0)
+    assert abs(float(dlam[0]) - total * ratio) <= (2.0 ** -8 + (chunks / 64 + 200) * 2.0 ** -24) * size * ratio
