@@ -740,9 +740,10 @@ __global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* parts, in
 
 // No rows at all: the states go through, and nothing adds to dlam.
 __global__ __launch_bounds__(256) void recur_none_kernel(const float* from, float* to, long long n, float* zero, int C) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (to && i < n) to[i] = from ? from[i] : 0.0f;
-    if (zero && i < C) zero[i] = 0.0f;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        if (to) to[i] = from ? from[i] : 0.0f;
+        if (zero && i < C) zero[i] = 0.0f;
+    }
 }
 
 // ---- one token per sequence.  One row and 256 V channels per workgroup.  A slot that stands at several rows is done by the
@@ -857,9 +858,8 @@ void by_chunks(const RecurPlan& q, Launch launch) {
 }
 
 int launch_none(const RecurArgs& a, const float* from, float* to, float* zero, hipStream_t stream) {
-    const long long n = (long long)a.S * a.C, blocks = ((n > a.C ? n : a.C) + 255) / 256;
-    if (!launch_fits(blocks, 256)) return SCAN2D_ERR_BAD_SHAPE;
-    hipLaunchKernelGGL(recur_none_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, from, to, n, zero, a.C);
+    const long long n = (long long)a.S * a.C, blocks = (n + 255) / 256, most = 1 << 16;      // S >= 1: n values are C at least
+    hipLaunchKernelGGL(recur_none_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, stream, from, to, n, zero, a.C);
     return launched();
 }
 

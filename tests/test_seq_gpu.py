@@ -884,3 +884,22 @@ def test_recurrence_of_as_many_rows_as_there_may_be(torch, s2d):
         total, size = total + float(q.sum()), size + float(q.abs().sum())
     ratio = 0.5 / np.log(2.0)                                                  # sigmoid(0) / softplus(0)
     assert abs(float(dlam[0]) - total * ratio) <= (2.0 ** -8 + (chunks / 64 + 200) * 2.0 ** -24) * size * ratio
+
+
+def test_recurrence_of_no_rows_with_many_states(torch, s2d):
+    """2^32 states and more go through a call of no rows, forward and backward."""
+    S, C = 2 ** 16 + 1, 2 ** 16
+    x, lam = torch.empty((0, C), device="cuda"), torch.zeros(C, device="cuda")
+    off = torch.zeros(S + 1, dtype=torch.int32, device="cuda")
+    h0 = torch.empty((S, C), device="cuda").uniform_()
+    _, hT, saved = s2d.seq_recur_fwd(x, x, x, lam, offsets=off, h0=h0, want_final=True, want_saved=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(hT[k:k + 4096], h0[k:k + 4096]) for k in range(0, S, 4096))
+    del hT
+    *_, dlam, dh0 = s2d.seq_recur_bwd(x, x, x, lam, x, saved, offsets=off, dhT=h0, want_dh0=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(dh0[k:k + 4096], h0[k:k + 4096]) for k in range(0, S, 4096)) and bool((dlam == 0).all())
+    del dh0
+    _, hT, _ = s2d.seq_recur_fwd(x, x, x, lam, offsets=off, want_final=True)
+    torch.cuda.synchronize()
+    assert all(not bool(hT[k:k + 4096].any()) for k in range(0, S, 4096))
