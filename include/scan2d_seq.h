@@ -86,7 +86,7 @@ int scan2d_seq_recur_bwd(const scan2d_recur_desc* desc, const void* x, const voi
  *     state[slot,c] = a_t * state[slot,c] + sqrt(1 - a_t^2) * sigmoid(i) * x,       h[t,c] = state[slot,c]
  *   state : [slot_count][C] fp32;  slots : [T] int32 or NULL.  A row whose slot is negative or not below slot_count is
  *   padding: its h is not written and no state changes.  A slot that stands at several rows takes them in the order of the rows,
- *   as one call after the other would.  1 <= T <= 65535.
+ *   as one call after the other would.  1 <= T <= 65535 and T ceil(C / 512) < 2^24 (one launch).
  */
 int scan2d_seq_recur_step(const scan2d_recur_desc* desc, const void* x, const void* r, const void* i, const float* lam,
                           float* state, const int32_t* slots, int64_t slot_count, void* h, void* stream);

@@ -906,15 +906,17 @@ int recur_bwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t
     return launched();
 }
 
+// One channel per lane where a workgroup has the row then.
+static int step_channels(const scan2d_recur_desc* d) { return d->C <= 256 ? 1 : 2; }
+static long long step_blocks(const scan2d_recur_desc* d) { return (d->C + 256LL * step_channels(d) - 1) / (256 * step_channels(d)) * d->T; }
+bool recur_step_fits(const scan2d_recur_desc* d) { return launch_fits(step_blocks(d), 256); }
 int recur_step_launch(const scan2d_recur_desc* d, const RecurArgs& a, float* state, const int32_t* slots, long long slot_count, hipStream_t stream) {
-    const int V = a.C <= 256 ? 1 : 2;                       // one channel per lane where a workgroup has the row then
-    const long long blocks = (long long)((a.C + 256 * V - 1) / (256 * V)) * a.T;
-    if (!launch_fits(blocks, 256)) return SCAN2D_ERR_BAD_SHAPE;
+    const int V = step_channels(d);
     (void)hipGetLastError();
     using Kernel = void (*)(const RecurArgs, float*, const int32_t*, long long);
     const Kernel k = d->dtype == SCAN2D_BF16 ? (V == 1 ? recur_step_kernel<bf16_t, 1> : recur_step_kernel<bf16_t, 2>)
                                              : (V == 1 ? recur_step_kernel<float, 1> : recur_step_kernel<float, 2>);
-    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, stream, a, state, slots, slot_count);
+    hipLaunchKernelGGL(k, dim3((unsigned)step_blocks(d)), dim3(256), 0, stream, a, state, slots, slot_count);
     return launched();
 }
 

@@ -27,6 +27,7 @@ size_t recur_saved_bytes(const scan2d_recur_desc* d);
 size_t recur_workspace_bytes(const scan2d_recur_desc* d, int pass);
 int recur_fwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t stream);
 int recur_bwd_launch(const scan2d_recur_desc* d, const RecurArgs& a, hipStream_t stream);
+bool recur_step_fits(const scan2d_recur_desc* d);        // below 2^32 threads
 int recur_step_launch(const scan2d_recur_desc* d, const RecurArgs& a, float* state, const int32_t* slots, long long slot_count, hipStream_t stream);
 
 struct GroupNormArgs {

@@ -142,7 +142,7 @@ extern "C" int scan2d_seq_recur_step(const scan2d_recur_desc* desc, const void* 
                                      const int32_t* slots, int64_t slot_count, void* h, void* stream) {
     int rc = check_recur(desc, false);
     if (rc != SCAN2D_OK) return rc;
-    if (desc->T < 1 || desc->T > 65535 || slot_count < 1 || slot_count >= (1LL << 31) || (slots == nullptr && slot_count < desc->T)) return SCAN2D_ERR_BAD_SHAPE;
+    if (desc->T < 1 || desc->T > 65535 || !recur_step_fits(desc) || slot_count < 1 || slot_count >= (1LL << 31) || (slots == nullptr && slot_count < desc->T)) return SCAN2D_ERR_BAD_SHAPE;
     if (!x || !r || !i || !lam || !state || !h) return SCAN2D_ERR_NULL_POINTER;
     const size_t e = elem_bytes(desc->dtype);
     if (!aligned(x, e) || !aligned(r, e) || !aligned(i, e) || !aligned(h, e) || !aligned(lam, 4) || !aligned(state, 4) || !aligned(slots, 4))

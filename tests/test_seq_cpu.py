@@ -231,3 +231,11 @@ def test_binding_takes_the_layouts_of_rows(lib):
         if x.dim() >= 3:
             with pytest.raises(ValueError, match="device tensor"):
                 lib.group_norm_fwd(x, None, None, 2)
+
+
+@pytest.mark.parametrize("T,C,fits", [(65535, 130560, True), (65535, 131072, True), (65535, 131073, False), (512, (1 << 24) - 1, False), (511, (1 << 24) - 1, True),
+                                      (1, (1 << 24) - 1, True), (65535, 1, True)])
+def test_step_is_refused_where_its_launch_would_hold_too_many_threads(lib, T, C, fits):
+    """T ceil(C / 512) below 2^24, looked at before the pointers."""
+    code = lib.lib.scan2d_seq_recur_step(ctypes.byref(_recur(lib, T=T, C=C)), None, None, None, OK, OK, OK, 8, OK, None)
+    assert code == (-1 if fits else -2)
