@@ -6,9 +6,9 @@
 //
 // Held form (group_norm_fwd_kernel, group_norm_bwd_kernel): a team of lanes holds all positions of an item's slab in
 // registers as they were loaded: one read.  Teams are a power of two of lanes within a wavefront (nothing waits for another
-// wavefront; a single token's groups, small maps), or a workgroup.  A team goes on to the next items of its slab with its
-// channels' parameters, and in the backward pass its channels' sums, in registers; where an item is one row of a lane, it takes
-// several items at once, so that enough bytes are on their way.
+// wavefront; small maps), or a workgroup.  A team goes on to the next items of its slab with its channels' parameters, and in the
+// backward pass its channels' sums, in registers; where an item is one row of a lane, a workgroup takes several items at once, so
+// that enough bytes are on their way.
 // Split form, where an item's slab does not fit: a workgroup has a tile, a share of an item's positions, and goes through it kRows rows
 // of a lane at a time.  Forward: each lane keeps mean and squared deviations of its channels (rows in registers: their mean, the deviations
 // from it, joined to those before by M2 = M2_1 + M2_2 + n1 n2 / (n1 + n2) (mean_1 - mean_2)^2), which are joined to those of the tile, those
@@ -1161,7 +1161,7 @@ constexpr int kMaxWgs = 2048;            // workgroups of the held form: eight p
 constexpr int kTileWgs = 512;            // tiles of the split form, at least, where there are rows enough: two per compute unit
 enum { FORM_WAVE = 0, FORM_GROUP = 1, FORM_SPLIT = 2, FORM_TOKENS = 3 };
 constexpr int kHeldRows = 8, kWaveThreads = 256, kGroupThreads = 512;
-constexpr int kItems = 4, kItemsBwd = 2;                   // single rows that a lane takes at once
+constexpr int kItems = 4, kItemsBwd = 2;                   // items of a workgroup that takes several at once, one row of a lane each
 constexpr int kTokenChannels = 2048;                       // of a group, at most: 32 a lane
 constexpr int kTokenWgs = 1024;                            // four workgroups of single rows per compute unit
 
@@ -1213,7 +1213,8 @@ NormPlan plan_of(const scan2d_group_norm_desc* d, bool backward) {
     n.one = D % n.V == 0;
     const auto held = [&](int form, long long most_teams) {
         n.form = form;
-        n.K = n.q.slots >= d->P && n.V > 1 ? 1 : kHeldRows;
+        // one row of a lane: a workgroup's only, since the fewest lanes of a wavefront that hold several positions hold them in several rows
+        n.K = form == FORM_GROUP && n.q.slots >= d->P && n.V > 1 ? 1 : kHeldRows;
         most_teams = most_teams < n.q.slabs ? n.q.slabs : most_teams / n.q.slabs * n.q.slabs;
         n.teams = (long long)d->N * n.q.slabs;
         if (n.teams > most_teams) n.teams = most_teams;
@@ -1298,8 +1299,8 @@ int fwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     if constexpr (V > 1)
         if (n.K == 1) {
             // one item per team: none that it could take besides
-            if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
-            else k = wave ? group_norm_fwd_kernel<T, V, ONE, 1, kItems, kWaveThreads, true, ACT> : group_norm_fwd_kernel<T, V, ONE, 1, kItems, kGroupThreads, false, ACT>;
+            if (n.teams >= (long long)a.N * n.q.slabs) k = group_norm_fwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
+            else k = group_norm_fwd_kernel<T, V, ONE, 1, kItems, kGroupThreads, false, ACT>;
         }
     const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams);
@@ -1331,8 +1332,8 @@ int bwd_held(const GroupNormArgs& a, const NormPlan& n, hipStream_t stream) {
     Kernel k = wave ? group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, kHeldRows, 1, kGroupThreads, false, ACT>;
     if constexpr (V > 1)
         if (n.K == 1) {
-            if (n.teams >= (long long)a.N * n.q.slabs) k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, 1, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
-            else k = wave ? group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kWaveThreads, true, ACT> : group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kGroupThreads, false, ACT>;
+            if (n.teams >= (long long)a.N * n.q.slabs) k = group_norm_bwd_kernel<T, V, ONE, 1, 1, kGroupThreads, false, ACT>;
+            else k = group_norm_bwd_kernel<T, V, ONE, 1, kItemsBwd, kGroupThreads, false, ACT>;
         }
     const long long blocks = wave ? (n.teams * n.q.ts + kWaveThreads - 1) / kWaveThreads : n.teams;
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(wave ? kWaveThreads : kGroupThreads), 0, stream, a, n.q, (int)n.teams, parts);
