@@ -12,6 +12,9 @@
  * least C and below 2^26 (0 stands for C), so that the halves of a projection [T][2 C] are used where they lie.  These tensors need
  * the alignment of their element type only; all others (parameters, states, statistics: dense) that of their type,
  * `saved` and `workspace` 16 bytes.
+ *
+ * Sizes: what is given at each descriptor.  A launch holds fewer than 2^32 threads; calls that need more are several launches
+ * (seq_recur_step alone is always one).
  */
 #ifndef SCAN2D_SEQ_H_
 #define SCAN2D_SEQ_H_

@@ -768,7 +768,7 @@ struct Tile {
     }
 };
 // kRows rows of a lane from r on: their masks, and what the ones that count hold (the others are not read: 65536 x 256 bf16 with half of
-// the positions masked, forward and backward 74 us where all are read, 66 so).  A batch's masks are asked for a batch ahead.
+// the positions masked, forward and backward 74 us where all are read, 64 so).  A batch's masks are asked for a batch ahead.
 template <bool MASK>
 struct Rows {
     uint8_t mask[kRows];

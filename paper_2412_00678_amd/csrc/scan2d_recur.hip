@@ -42,7 +42,7 @@ __device__ __forceinline__ float decay_of(float lam, float scale) { return scale
 __device__ __forceinline__ float decay_slope(float lam) { return lam < -15.0f ? 1.0f : 1.0f / ((1.0f + expf(-lam)) * (lam > 20.0f ? lam : log1pf(expf(lam)))); }
 
 // 1 - 2^(2y) for y <= 0 without the cancellation near 0, a = 2^y: -y p(y), p the Chebyshev fit of degree 5 to
-// (1 - 2^(2y)) / -y on [-0.5, 0] (off by 1.1e-8); beyond, 1 - a^2 >= 0.5 loses nothing.
+// (1 - 2^(2y)) / -y on [-0.5, 0] (off by 2.5e-8 with the constants as rounded to fp32); beyond, 1 - a^2 >= 0.5 loses nothing.
 __device__ __forceinline__ float one_minus_square(float y, float a) {
     float p = fmaf(y, 0.007358775474131107f, 0.0413372628390789f);
     p = fmaf(y, p, 0.15355470776557922f);
